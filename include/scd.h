@@ -275,6 +275,56 @@ int scd_lm_head_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
  * (d_z fp32 [B, L, n], window order) instead of computed by the LM head. */
 int scd_step_logits(scd_ctx* ctx, const float* d_z, void* d_state);
 
+/* ---- the vocabulary table at the model's other end, and what it learns -------------------------
+ * The same table W, bf16 bits [V, d] row-major, all pointers 16-byte aligned (d_ids, d_targets and the
+ * float arrays 4-byte).  All of them need cfg.d > 0; of the rest of the configuration they use what is
+ * named below, so a context with B = L = N = 1 serves a program that decodes nothing.  `rows` = 0 is allowed (arrays of
+ * no elements may then be NULL).  Workspaces are the caller's, 256-byte aligned, of the size that the
+ * query gives for the same arguments (0 for bad ones); nothing in one outlives the call.  Calls on different
+ * streams, contexts or in different recorded graphs must not share one if they may overlap in time. */
+
+/* Type of a gradient of W. */
+typedef enum scd_grad_type {
+  SCD_GRAD_BF16 = 0,
+  SCD_GRAD_F32 = 1
+} scd_grad_type;
+
+/* x[r] = scale * W[id_r], rounded once.  d_ids int32 [rows], ids of the whole vocabulary (not offsets); an id outside
+ * [0, V) (padding) gives zeros.  d_x bf16 [rows, d], written. */
+int scd_embed(scd_ctx* ctx, const int32_t* d_ids, int32_t rows, const uint16_t* d_W, float scale, uint16_t* d_x);
+
+/* The same for the drafts in the decode state, as the model reads them before the next scd_step: d_x bf16
+ * [B, C, L, d] as d_h there, row s of a sequence <-> position i_b + s, zeros for rows past the sequence's end; with
+ * guidance the uncond rows get the same. */
+int scd_embed_window(scd_ctx* ctx, const void* d_state, const uint16_t* d_W, float scale, uint16_t* d_x);
+
+/* Gradient of scd_embed with respect to W: d_dW[v] = scale * sum of d_dx[r] over the rows with id_r = v, added up in 32
+ * bits in an order that depends on the ids alone (the same call gives the same bits), rounded once.
+ *   d_dx bf16 [rows, d];  d_dW [V, d] of type grad_type: with accumulate = 0 every row is written (zeros where no id
+ * points), with accumulate = 1 the sum is added to the rows that occur, the others are left alone. */
+size_t scd_embed_backward_workspace_bytes(const scd_config* cfg, int32_t rows);
+int scd_embed_backward(scd_ctx* ctx, const int32_t* d_ids, int32_t rows, const uint16_t* d_dx, float scale, void* d_dW,
+                       int32_t grad_type, int32_t accumulate, void* d_workspace, size_t workspace_bytes);
+
+/* Softmax cross entropy of hidden rows over the allowed ids, without forming the logits in memory:
+ *   z = h W^T / tau (allowed rows of W),  lse = log sum exp(z),  loss = lse - z[target].
+ * top_k, top_p and the decode options do not enter; cfg_lambda must be 0 (SCD_EUNSUPPORTED otherwise).
+ *   d_h bf16 [rows, d];  d_targets int32 [rows], OFFSETS into the allowed ids; a negative one leaves the row out (loss 0,
+ * no gradient, whatever the row holds), one of n or more is not an allowed id (loss +inf, gradient of the normaliser alone);
+ *   d_loss, d_lse fp32 [rows], written.  rows up to 2^20. */
+size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows);
+int scd_cross_entropy(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
+                      float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes);
+
+/* Its gradient.  d_lse from scd_cross_entropy on the same arguments; d_weight fp32 [rows], the gradient of the result with
+ * respect to each row's loss, NULL = 1 (1 / rows for a mean).  The logits are made again, a piece of the vocabulary at a
+ * time.  d_dh bf16 [rows, d] and d_dW [V, d] of type grad_type, of which the allowed rows alone are written, or added to
+ * with accumulate = 1 (in 32 bits, rounded once); either may be NULL (not wanted).  The same call gives the same bits. */
+size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type);
+int scd_cross_entropy_backward(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
+                               const float* d_lse, const float* d_weight, uint16_t* d_dh, void* d_dW, int32_t grad_type,
+                               int32_t accumulate, void* d_workspace, size_t workspace_bytes);
+
 /* Synchronises the stream and reports: host_flags[0] = numeric-fault bits,
  * host_flags[1] = 1 if every sequence has emitted N tokens, host_flags[2] =
  * largest t_b, host_flags[3] = 0.  Returns SCD_ENUMERIC if a fault bit is set. */

@@ -80,6 +80,18 @@ def load():
     lib.scd_step_logits.argtypes = [vp, vp, vp]
     lib.scd_set_lm_head_events.argtypes = [vp, vp, vp]
     lib.scd_lm_head_kernel_name.argtypes = [vp, ctypes.c_char_p, sz]
+    f32 = ctypes.c_float
+    lib.scd_embed.argtypes = [vp, vp, i32, vp, f32, vp]
+    lib.scd_embed_window.argtypes = [vp, vp, vp, f32, vp]
+    lib.scd_embed_backward_workspace_bytes.restype = sz
+    lib.scd_embed_backward_workspace_bytes.argtypes = [cfgp, i32]
+    lib.scd_embed_backward.argtypes = [vp, vp, i32, vp, f32, vp, i32, i32, vp, sz]
+    lib.scd_cross_entropy_workspace_bytes.restype = sz
+    lib.scd_cross_entropy_workspace_bytes.argtypes = [cfgp, i32]
+    lib.scd_cross_entropy.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, sz]
+    lib.scd_cross_entropy_backward_workspace_bytes.restype = sz
+    lib.scd_cross_entropy_backward_workspace_bytes.argtypes = [cfgp, i32, i32]
+    lib.scd_cross_entropy_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, sz]
     lib.scd_status.argtypes = [vp, vp, ctypes.POINTER(i32 * 4)]
     lib.scd_strerror.restype = ctypes.c_char_p
     lib.scd_strerror.argtypes = [ctypes.c_int]
@@ -87,7 +99,8 @@ def load():
     lib.scdw_copy.argtypes = [vp, vp, vp, sz]
     for name in ("scd_create", "scd_destroy", "scd_reset", "scd_state_field", "scd_lm_head",
                  "scd_select", "scd_couple_draft", "scd_couple_draft_static", "scd_verify", "scd_step", "scd_step_logits",
-                 "scd_set_lm_head_events", "scd_lm_head_kernel_name",
+                 "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_embed", "scd_embed_window",
+                 "scd_embed_backward", "scd_cross_entropy", "scd_cross_entropy_backward",
                  "scd_status", "scdw_gather_hidden", "scdw_copy"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -128,6 +141,14 @@ def _ptr(t, dtypes, numel, what):
 
 
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+GRAD_BF16, GRAD_F32 = 0, 1
+_GRAD = {torch.bfloat16: GRAD_BF16, torch.float32: GRAD_F32}
+
+
+def _grad_type(dtype):
+    if dtype not in _GRAD:
+        raise TypeError(f"gradient of W: dtype {dtype}, expected one of {tuple(_GRAD)}")
+    return _GRAD[dtype]
 
 
 class Scd:
@@ -254,6 +275,65 @@ class Scd:
         self._check(self.lib.scd_step_logits(
             self.ctx, _ptr(z, (torch.float32,), c.B * c.L * self.n, "z"),
             _ptr(state, (torch.uint8,), state_bytes(c), "state")), "scd_step_logits")
+
+    # -- the vocabulary table at the model's other end, and what it learns ----------
+    def _workspace(self, need, what):
+        if need == 0:
+            raise ScdError(SCD_EINVAL, what)
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def embed(self, ids, W, scale, x):
+        """x[r] = scale * W[ids[r]] for every id of `ids`; zeros for ids outside [0, V)."""
+        c, rows = self.cfg, ids.numel()
+        self._check(self.lib.scd_embed(
+            self.ctx, _ptr(ids, (torch.int32,), rows, "ids"), rows, _ptr(W, _BF16, c.V * c.d, "W"), float(scale),
+            _ptr(x, _BF16, rows * c.d, "x")), "scd_embed")
+
+    def embed_window(self, state, W, scale, x):
+        c = self.cfg
+        self._check(self.lib.scd_embed_window(
+            self.ctx, _ptr(state, (torch.uint8,), state_bytes(c), "state"), _ptr(W, _BF16, c.V * c.d, "W"), float(scale),
+            _ptr(x, _BF16, c.B * self.C * c.L * c.d, "x")), "scd_embed_window")
+
+    def embed_backward_workspace(self, rows):
+        return self._workspace(self.lib.scd_embed_backward_workspace_bytes(ctypes.byref(self.cfg), rows),
+                               "scd_embed_backward_workspace_bytes")
+
+    def embed_backward(self, ids, dx, scale, dW, workspace, accumulate=False):
+        """dW (bf16 or fp32) = or += scale * the sums of dx's rows by id."""
+        c, rows = self.cfg, ids.numel()
+        self._check(self.lib.scd_embed_backward(
+            self.ctx, _ptr(ids, (torch.int32,), rows, "ids"), rows, _ptr(dx, _BF16, rows * c.d, "dx"), float(scale),
+            _ptr(dW, tuple(_GRAD), c.V * c.d, "dW"), _grad_type(dW.dtype), int(accumulate),
+            _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()), "scd_embed_backward")
+
+    def cross_entropy_workspace(self, rows):
+        return self._workspace(self.lib.scd_cross_entropy_workspace_bytes(ctypes.byref(self.cfg), rows),
+                               "scd_cross_entropy_workspace_bytes")
+
+    def cross_entropy(self, h, W, targets, loss, lse, workspace):
+        """One loss and log normaliser per target; a negative target leaves its row out."""
+        c, rows = self.cfg, targets.numel()
+        self._check(self.lib.scd_cross_entropy(
+            self.ctx, _ptr(h, _BF16, rows * c.d, "h"), _ptr(W, _BF16, c.V * c.d, "W"),
+            _ptr(targets, (torch.int32,), rows, "targets"), rows, _ptr(loss, (torch.float32,), rows, "loss"),
+            _ptr(lse, (torch.float32,), rows, "lse"), _ptr(workspace, (torch.uint8,), 1, "workspace"),
+            workspace.numel()), "scd_cross_entropy")
+
+    def cross_entropy_backward_workspace(self, rows, grad_dtype=torch.bfloat16):
+        return self._workspace(self.lib.scd_cross_entropy_backward_workspace_bytes(
+            ctypes.byref(self.cfg), rows, _grad_type(grad_dtype)), "scd_cross_entropy_backward_workspace_bytes")
+
+    def cross_entropy_backward(self, h, W, targets, lse, weight, dh, dW, workspace, accumulate=False):
+        """Gradients of sum(weight * loss) (weight None: 1); dh or dW may be None."""
+        c, rows = self.cfg, targets.numel()
+        self._check(self.lib.scd_cross_entropy_backward(
+            self.ctx, _ptr(h, _BF16, rows * c.d, "h"), _ptr(W, _BF16, c.V * c.d, "W"),
+            _ptr(targets, (torch.int32,), rows, "targets"), rows, _ptr(lse, (torch.float32,), rows, "lse"),
+            _ptr(weight, (torch.float32,), rows, "weight"), _ptr(dh, _BF16, rows * c.d, "dh"),
+            _ptr(dW, tuple(_GRAD), c.V * c.d, "dW"), _grad_type(dW.dtype) if dW is not None else GRAD_BF16,
+            int(accumulate), _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()),
+            "scd_cross_entropy_backward")
 
     # -- benchmark plumbing ---------------------------------------------------
     def gather_hidden(self, table, age_cap, state, h):

@@ -356,6 +356,25 @@ int couple_draft_impl(scd_ctx* c, char* w, bool cands, const float* d_z_cur, con
   return hip_rc(scd::launch_row(ra, c->stream, c->row_lds));
 }
 
+// What the operators on the vocabulary table check alike.
+constexpr int32_t kCrossEntropyRows = 1 << 20;
+inline bool valid_gradient(int32_t grad_type, int32_t accumulate) {
+  return (grad_type == SCD_GRAD_BF16 || grad_type == SCD_GRAD_F32) && (accumulate == 0 || accumulate == 1);
+}
+inline bool valid_workspace(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
+
+int cross_entropy_args(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
+                       scd::CrossEntropyArgs* a) {
+  if (!d_W || rows < 0 || rows > kCrossEntropyRows || (rows > 0 && (!d_h || !d_targets)) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!aligned(d_h, 16) || !aligned(d_W, 16) || !aligned(d_targets, 4)) return SCD_EINVAL;
+  if (c->C != 1) return SCD_EUNSUPPORTED;
+  a->h = d_h;
+  a->W = d_W + static_cast<size_t>(c->cfg.v_lo) * c->cfg.d;
+  a->targets = d_targets;
+  a->rows = rows; a->n = c->n; a->d = c->cfg.d; a->tau = c->cfg.temperature;
+  return SCD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -470,6 +489,88 @@ int scd_lm_head_kernel_name(scd_ctx* c, char* host_buf, size_t cap) {
 int scd_step_logits(scd_ctx* c, const float* d_z, void* st) {
   if (!c || !d_z || !st || !aligned(st, kAlign)) return SCD_EINVAL;
   return run_tail(c, st, 0, d_z);
+}
+
+// ---- operators on the vocabulary table ---------------------------------------------------
+size_t scd_embed_backward_workspace_bytes(const scd_config* cfg, int32_t rows) {
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0) return 0;
+  return scd::embed_backward_bytes(rows, cfg->d);
+}
+
+int scd_embed(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uint16_t* d_W, float scale, uint16_t* d_x) {
+  if (!c || !d_W || rows < 0 || (rows > 0 && (!d_ids || !d_x)) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!aligned(d_ids, 4) || !aligned(d_W, 16) || !aligned(d_x, 16)) return SCD_EINVAL;
+  scd::EmbedArgs a{};
+  a.ids = d_ids; a.W = d_W; a.x = d_x;
+  a.rows = rows; a.V = c->cfg.V; a.d = c->cfg.d; a.scale = scale;
+  return hip_rc(scd::launch_embed(a, c->stream));
+}
+
+int scd_embed_window(scd_ctx* c, const void* d_state, const uint16_t* d_W, float scale, uint16_t* d_x) {
+  if (!c || !d_state || !d_W || !d_x || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!aligned(d_state, kAlign) || !aligned(d_W, 16) || !aligned(d_x, 16)) return SCD_EINVAL;
+  const int64_t rows = static_cast<int64_t>(c->cfg.B) * c->C * c->cfg.L;
+  if (rows > INT32_MAX) return SCD_EUNSUPPORTED;
+  void* const st = const_cast<void*>(d_state);
+  scd::EmbedArgs a{};
+  a.W = d_W; a.x = d_x;
+  a.rows = static_cast<int>(rows); a.V = c->cfg.V; a.d = c->cfg.d; a.scale = scale;
+  a.X = field<int32_t>(c, st, SCD_F_X);
+  a.pos = field<int32_t>(c, st, SCD_F_POS);
+  a.C = c->C; a.L = c->cfg.L; a.N = c->cfg.N; a.v_lo = c->cfg.v_lo;
+  return hip_rc(scd::launch_embed(a, c->stream));
+}
+
+int scd_embed_backward(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uint16_t* d_dx, float scale, void* d_dW,
+                       int32_t grad_type, int32_t accumulate, void* d_workspace, size_t workspace_bytes) {
+  if (!c || !d_dW || rows < 0 || (rows > 0 && (!d_ids || !d_dx)) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!valid_gradient(grad_type, accumulate)) return SCD_EINVAL;
+  if (!aligned(d_ids, 4) || !aligned(d_dx, 16) || !aligned(d_dW, 16)) return SCD_EINVAL;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::embed_backward_bytes(rows, c->cfg.d))) return SCD_EWORKSPACE;
+  scd::EmbedBackwardArgs a{};
+  a.ids = d_ids; a.dx = d_dx; a.dW = d_dW;
+  a.rows = rows; a.V = c->cfg.V; a.d = c->cfg.d; a.scale = scale;
+  a.f32 = grad_type == SCD_GRAD_F32; a.accumulate = accumulate != 0;
+  a.ws = d_workspace;
+  return hip_rc(scd::launch_embed_backward(a, c->stream));
+}
+
+size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows) {
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows) return 0;
+  return scd::cross_entropy_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d);
+}
+
+size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type) {
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !valid_gradient(grad_type, 0)) return 0;
+  return scd::cross_entropy_backward_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d, grad_type == SCD_GRAD_F32);
+}
+
+int scd_cross_entropy(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
+                      float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes) {
+  if (!c || (rows > 0 && (!d_loss || !d_lse)) || !aligned(d_loss, 4) || !aligned(d_lse, 4)) return SCD_EINVAL;
+  scd::CrossEntropyArgs a{};
+  if (int rc = cross_entropy_args(c, d_h, d_W, d_targets, rows, &a); rc != SCD_OK) return rc;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::cross_entropy_bytes(rows, c->n, c->cfg.d))) return SCD_EWORKSPACE;
+  a.loss = d_loss; a.lse = d_lse; a.ws = d_workspace;
+  return hip_rc(scd::launch_cross_entropy(a, c->stream));
+}
+
+int scd_cross_entropy_backward(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
+                               const float* d_lse, const float* d_weight, uint16_t* d_dh, void* d_dW, int32_t grad_type,
+                               int32_t accumulate, void* d_workspace, size_t workspace_bytes) {
+  if (!c || (rows > 0 && !d_lse) || !aligned(d_lse, 4) || !aligned(d_weight, 4) || !aligned(d_dh, 16) || !aligned(d_dW, 16))
+    return SCD_EINVAL;
+  if (!valid_gradient(grad_type, accumulate)) return SCD_EINVAL;
+  scd::CrossEntropyArgs a{};
+  if (int rc = cross_entropy_args(c, d_h, d_W, d_targets, rows, &a); rc != SCD_OK) return rc;
+  const bool f32 = grad_type == SCD_GRAD_F32;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::cross_entropy_backward_bytes(rows, c->n, c->cfg.d, f32)))
+    return SCD_EWORKSPACE;
+  a.lse = const_cast<float*>(d_lse); a.weight = d_weight; a.dh = d_dh;
+  const size_t skip = static_cast<size_t>(c->cfg.v_lo) * c->cfg.d * (f32 ? 4 : 2);
+  a.dW = d_dW ? static_cast<char*>(d_dW) + skip : nullptr;
+  a.f32 = f32; a.accumulate = accumulate != 0; a.ws = d_workspace;
+  return hip_rc(scd::launch_cross_entropy_backward(a, c->stream));
 }
 
 int scd_status(scd_ctx* c, void* st, int32_t host_flags[4]) {

@@ -169,4 +169,50 @@ struct ResetArgs {
 };
 hipError_t launch_reset(const ResetArgs& a, hipStream_t s);
 
+// ---- operators on the vocabulary table beside the step ---------------------------
+struct EmbedArgs {
+  const int32_t* ids;   // [rows], or null: the drafts of the decode state's windows (the fields below)
+  const uint16_t* W;    // bf16 [V, d]
+  uint16_t* x;          // bf16 [rows, d]
+  int rows, V, d;
+  float scale;
+  const int32_t* X;     // [B, L] by slot; rows = B * C * L
+  const int32_t* pos;   // [B]
+  int C, L, N, v_lo;
+};
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t s);
+
+struct EmbedBackwardArgs {
+  const int32_t* ids;   // [rows]
+  const uint16_t* dx;   // bf16 [rows, d]
+  void* dW;             // [V, d], bf16 or fp32
+  int rows, V, d;
+  float scale;
+  bool f32, accumulate;
+  void* ws;             // embed_backward_bytes(rows, d), 256-byte aligned
+};
+size_t embed_backward_bytes(int rows, int d);
+hipError_t launch_embed_backward(const EmbedBackwardArgs& a, hipStream_t s);
+
+// Softmax cross entropy of hidden rows over the n columns that the rows of W stand for.
+struct CrossEntropyArgs {
+  const uint16_t* h;         // bf16 [rows, d]
+  const uint16_t* W;         // bf16 [n, d]: first allowed row of the table
+  const int32_t* targets;    // [rows]: columns; negative: the row is left out
+  int rows, n, d;
+  float tau;
+  float* loss;               // forward, [rows]
+  float* lse;                // [rows]: written by the forward pass, read by the backward pass
+  // backward
+  const float* weight;       // [rows] or null (1): gradient of the result with respect to the row's loss
+  uint16_t* dh;              // bf16 [rows, d] or null
+  void* dW;                  // [n, d] or null, bf16 or fp32
+  bool f32, accumulate;
+  void* ws;                  // cross_entropy_bytes / cross_entropy_backward_bytes, 256-byte aligned
+};
+size_t cross_entropy_bytes(int rows, int n, int d);
+hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t s);
+size_t cross_entropy_backward_bytes(int rows, int n, int d, bool f32);
+hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& a, hipStream_t s);
+
 }  // namespace scd
