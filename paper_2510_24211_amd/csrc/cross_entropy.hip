@@ -6,9 +6,14 @@
 //   Forward: a tile of logits leaves (maximum, sum of exponentials) per row and the target's logit; finish_kernel joins a
 // row's tiles.  Backward, for a piece of the vocabulary at a time: dz of the piece goes to the workspace as rows and as
 // columns (k lies along ids for dh, along rows for dW), the piece of W and the rows of h are turned once for the same reason.
-//   dz is rounded to bf16 for the matrix units: its terms err by up to 2^-8 of themselves, independently, as the bf16
-// results do.  Where dW is kept in 32 bits dz enters that product as two bf16 terms (16 bits of its mantissa), at the
-// price of a fifth product.  Statistics and sums are fp32.
+//   The products of the gradient take fp16 operands: dz has to be rounded for the matrix units, and bf16 would leave each of its
+// terms an error as large as that of the bf16 results (2^-9 of the term, at 515 rows x 16395 ids 0.0025 of dh in the mean
+// against 64 bits, where the rounding of the result alone makes 0.0017); fp16 errs by an eighth of it.  Its range is
+// short, so every operand is brought under 2^15 by a power of two: W and the rows of h by the exponent of their largest finite
+// element (range_kernel reads them once), dz, which lies in [-1, 1] without the rows' weights, by 2^14, and with
+// the weights for dW by the exponent of the largest.  The elements of W and h, of 8 bits, stay exact down to 2^-31 of the
+// largest; dz has its 11 bits down to 2^-28, and an absolute error of 2^-39 below.  Where dW is kept in 32 bits dz enters its product
+// as two terms (22 bits), at the price of a fifth product.  Statistics and sums are fp32.
 #include "gemm_tile.h"
 #include "scd_device.h"
 #include "scd_kernels.h"
@@ -33,6 +38,12 @@ __device__ __forceinline__ float half_fold(float v, F&& f) {
 
 enum GemmUse { kLoss, kGradient, kRows, kTable };
 
+// floor(log2) of the largest finite element of the allowed rows of W, of the rows of h and of the weights that count
+struct Exponents {
+  int W, h, weight;
+};
+constexpr int kTop = 14;     // operands of the gradient's products lie below 2^(kTop + 1)
+
 struct GemmArgs {
   const uint16_t* A;
   const uint16_t* B;
@@ -48,8 +59,8 @@ struct GemmArgs {
   float* zt;                 // [M]
   const float* lse;
   const float* weight;
-  uint16_t* dz;              // [M][ldz]
-  uint16_t* dzT;             // [N][ldT]: hi terms, then (two_terms) lo terms `lo` columns on
+  uint16_t* dz;              // fp16 [M][ldz], 2^14 times dz without the rows' weights
+  uint16_t* dzT;             // fp16 [N][ldT], with them: first terms, then (two_terms) the second ones `lo` columns on
   int64_t ldz, ldT;
   int lo;
   bool two_terms;
@@ -58,7 +69,13 @@ struct GemmArgs {
   bool first, last;
   void* out;
   bool f32, accumulate;
+  const Exponents* exps;
 };
+
+// what multiplies a row of dz W: 0 where the row is left out, whatever its weight
+__device__ __forceinline__ float row_factor(const int32_t* targets, const float* weight, float inv_tau, int row) {
+  return targets[row] < 0 ? 0.f : (weight ? weight[row] : 1.f) * inv_tau;
+}
 
 template <class K>
 constexpr int epilogue_bytes() {
@@ -72,6 +89,8 @@ constexpr int lds_bytes() {
 // element j of accumulator block i: this row of the wavefront's
 __device__ __forceinline__ int block_row(int i, int j, int lg) { return i * 32 + (j >> 2) * 8 + lg * 4 + (j & 3); }
 __device__ __forceinline__ uint16_t bf16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
+__device__ __forceinline__ uint16_t f16_bits(float v) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v)); }
+__device__ __forceinline__ float f16_value(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
 
 // The tile in LDS, `rows` lines of `cols` bf16 values (pitch cols + 8), to memory: lines below `line_end`, whole
@@ -112,7 +131,7 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
   const TileOperand B{reinterpret_cast<uint64_t>(a.B + col0 * a.ldb), cols, static_cast<uint32_t>(a.ldb * 2), a.wrapB};
   // the workgroups of an XCD meet in its L2, the XCDs start at different columns
   const int rot = KT > 0 ? static_cast<int>(static_cast<int64_t>(blockIdx.x % 8) * KT / 8) : 0;
-  multiply_tile<K>(lds, A, B, kt0, KT, a.tail, rot, acc);
+  multiply_tile<K, USE == kRows || USE == kTable>(lds, A, B, kt0, KT, a.tail, rot, acc);
   __syncthreads();
 
   if constexpr (USE == kLoss || USE == kGradient) {
@@ -124,7 +143,7 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
       target[r] = t < 0 ? -1 : t - a.col0 - col0 < 0 || t - a.col0 - col0 >= BN ? BN : t - a.col0 - col0;   // column of the tile
       if constexpr (USE == kGradient) {
         lse2[r] = r < rows ? a.lse[row0 + r] * kLog2e : 0.f;
-        coef[r] = (r < rows && a.weight ? a.weight[row0 + r] : 1.f) * a.inv_tau;
+        coef[r] = __builtin_ldexpf(r < rows && a.weight ? a.weight[row0 + r] : 1.f, -a.exps->weight);
       }
     }
     __syncthreads();
@@ -167,17 +186,17 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
       }
     } else {
       uint16_t* const tile = reinterpret_cast<uint16_t*>(lds + 16 * HR);
-      // dz replaces the logits
+      // 2^14 dz, without the row's weight, replaces the logits
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int r = wr * K::RW + block_row(i, j, lg), t = target[r];
-          const float l = lse2[r], g = coef[r];
+          const float l = lse2[r];
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
             const float p = exp2_fast(__builtin_fmaf(acc[c][i][j], a.scale2, -l));
-            const float v = g * (p - (t == c0 + c * 32 ? 1.f : 0.f));
+            const float v = (p - (t == c0 + c * 32 ? 1.f : 0.f)) * (1 << kTop);
             acc[c][i][j] = t < 0 || c0 + c * 32 >= cols ? 0.f : v;
           }
         }
@@ -188,13 +207,23 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
           for (int j = 0; j < 16; ++j)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-              tile[(wr * K::RW + block_row(i, j, lg)) * (BN + 8) + c0 + c * 32] = bf16_bits(acc[c][i][j]);
+              tile[(wr * K::RW + block_row(i, j, lg)) * (BN + 8) + c0 + c * 32] = f16_bits(acc[c][i][j]);
         __syncthreads();
         store_lines<HR, BN, K::THREADS>(tile, a.dz + row0 * a.ldz + col0, a.ldz, rows, static_cast<int>(a.ldz) - col0);
         __syncthreads();
       }
       if (a.dzT) {
         const int stretch = a.lo;                       // columns of one term
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int r = wr * K::RW + block_row(i, j, lg);
+            const bool there = target[r] >= 0;          // (a row that is left out may have any weight)
+            const float g = coef[r];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) acc[c][i][j] = there ? acc[c][i][j] * g : 0.f;
+          }
         for (int term = 0; term < (a.two_terms ? 2 : 1); ++term) {
 #pragma unroll
           for (int i = 0; i < NB; ++i)
@@ -205,8 +234,8 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
                 uint16_t b[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                  b[e] = bf16_bits(acc[c][i][4 * g + e]);
-                  acc[c][i][4 * g + e] -= bf16_value(b[e]);       // the rest, for the second term
+                  b[e] = f16_bits(acc[c][i][4 * g + e]);
+                  acc[c][i][4 * g + e] -= f16_value(b[e]);       // the rest, for the second term
                 }
                 *reinterpret_cast<uint2*>(tile + (c0 + c * 32) * (HR + 8) + wr * K::RW + i * 32 + g * 8 + lg * 4) =
                     make_uint2(b[0] | static_cast<uint32_t>(b[1]) << 16, b[2] | static_cast<uint32_t>(b[3]) << 16);
@@ -237,6 +266,23 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
           }
         if (!a.last) return;
       }
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int r = min(wr * K::RW + block_row(i, j, lg), rows - 1);
+          const float f = row_factor(a.targets, a.weight, a.inv_tau, row0 + r);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) acc[c][i][j] = __builtin_ldexpf(acc[c][i][j], a.exps->W - 2 * kTop) * f;
+        }
+    } else {
+      const int e = a.exps->h + a.exps->weight - 2 * kTop;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) acc[c][i][j] = __builtin_ldexpf(acc[c][i][j] * a.inv_tau, e);
     }
     if (a.f32 || a.accumulate) {
 #pragma unroll
@@ -303,13 +349,76 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
   }
 }
 
-// ---- to[c][r] = from[r][c] for r < rows, 0 for r up to rows_pad and for rows with a negative mark --------
+// ---- the largest elements ----------------------------------------------------------------------------
+// Per workgroup the largest magnitude (as an integer: the order is the same) among the finite elements of its share of W,
+// of the rows of h and of their weights; settle_kernel takes the largest of those.
+constexpr int kRangeBlocks = 1024;
+__device__ __forceinline__ uint32_t finite_magnitude16(uint32_t two) {            // the larger of two bf16 values'
+  const uint32_t a = two & 0x7FFFu, b = two >> 16 & 0x7FFFu;
+  return max(a < 0x7F80u ? a : 0u, b < 0x7F80u ? b : 0u);
+}
+__device__ __forceinline__ uint32_t finite_magnitude16(u32x4 v) {
+  return max(max(finite_magnitude16(v[0]), finite_magnitude16(v[1])), max(finite_magnitude16(v[2]), finite_magnitude16(v[3])));
+}
+template <int NW>
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* words) {
+  v = wave_max_u32(v);
+  if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0u;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) v = max(v, words[w]);
+  __syncthreads();
+  return v;
+}
+__global__ __launch_bounds__(256) void range_kernel(const u32x4* __restrict__ W, int64_t pieces_W, const u32x4* __restrict__ h, int rows, int d8,
+                                                    const float* __restrict__ weight, const int32_t* __restrict__ targets,
+                                                    uint3* __restrict__ out) {
+  __shared__ uint32_t words[4];
+  uint32_t w = 0u, x = 0u, g = 0u;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256, first = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  constexpr int AHEAD = 8;
+  for (int64_t i = first; i < pieces_W; i += AHEAD * step) {
+    u32x4 v[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) v[k] = W[min(i + k * step, pieces_W - 1)];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) w = max(w, finite_magnitude16(v[k]));
+  }
+  for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+    if (targets[r] < 0) continue;
+    for (int i = threadIdx.x; i < d8; i += 256) x = max(x, finite_magnitude16(h[static_cast<int64_t>(r) * d8 + i]));
+    const uint32_t m = weight ? __float_as_uint(weight[r]) & 0x7FFFFFFFu : 0x3F800000u;
+    g = max(g, m < 0x7F800000u ? m : 0u);
+  }
+  w = block_max<4>(w, words);
+  x = block_max<4>(x, words);
+  g = block_max<4>(g, words);
+  if (threadIdx.x == 0) out[blockIdx.x] = make_uint3(w, x, g);
+}
+__global__ __launch_bounds__(256) void settle_kernel(const uint3* __restrict__ in, int blocks, Exponents* __restrict__ out) {
+  __shared__ uint32_t words[4];
+  uint32_t w = 0u, x = 0u, g = 0u;
+  for (int i = threadIdx.x; i < blocks; i += 256) {
+    const uint3 v = in[i];
+    w = max(w, v.x);
+    x = max(x, v.y);
+    g = max(g, v.z);
+  }
+  w = block_max<4>(w, words);
+  x = block_max<4>(x, words);
+  g = block_max<4>(g, words);
+  if (threadIdx.x == 0)
+    *out = Exponents{static_cast<int>(w >> 7) - 127, static_cast<int>(x >> 7) - 127, static_cast<int>(g >> 23) - 127};
+}
+
+// ---- to[c][r] = from[r][c] * 2^(kTop - exponent) in fp16 for r < rows, 0 for r up to rows_pad and where marks[r] < 0 ------
 constexpr int kTurn = 64;
 __global__ __launch_bounds__(256) void turn_kernel(const uint16_t* __restrict__ from, int64_t ld_from, int rows, int cols,
                                                    uint16_t* __restrict__ to, int64_t ld_to, int rows_pad,
-                                                   const int32_t* __restrict__ marks) {
+                                                   const int32_t* __restrict__ marks, const int* __restrict__ exponent) {
   __shared__ uint16_t tile[kTurn][kTurn + 2];
-  const int r0 = blockIdx.x * kTurn, c0 = blockIdx.y * kTurn;
+  const int r0 = blockIdx.x * kTurn, c0 = blockIdx.y * kTurn, up = kTop - *exponent;
   for (int p = threadIdx.x; p < kTurn * kTurn / 8; p += 256) {
     const int r = p / (kTurn / 8), c = p % (kTurn / 8) * 8;
     u32x4 v{0u, 0u, 0u, 0u};
@@ -317,7 +426,9 @@ __global__ __launch_bounds__(256) void turn_kernel(const uint16_t* __restrict__ 
       v = *reinterpret_cast<const u32x4*>(from + static_cast<int64_t>(r0 + r) * ld_from + c0 + c);
     uint32_t* const at = reinterpret_cast<uint32_t*>(&tile[r][c]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) at[e] = v[e];
+    for (int e = 0; e < 4; ++e)
+      at[e] = f16_bits(__builtin_ldexpf(bf16_value(v[e] & 0xFFFFu), up)) |
+              static_cast<uint32_t>(f16_bits(__builtin_ldexpf(bf16_value(v[e] >> 16), up))) << 16;
   }
   __syncthreads();
   for (int p = threadIdx.x; p < kTurn * kTurn / 8; p += 256) {
@@ -331,16 +442,22 @@ __global__ __launch_bounds__(256) void turn_kernel(const uint16_t* __restrict__ 
 }
 
 // ---- dh from the parts of k ------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void join_rows_kernel(const float* __restrict__ sums, int parts, int64_t count, uint16_t* __restrict__ out) {
+__global__ __launch_bounds__(256) void join_rows_kernel(const float* __restrict__ sums, int parts, int64_t count, int d,
+                                                        const int32_t* __restrict__ targets, const float* __restrict__ weight, float inv_tau,
+                                                        const Exponents* __restrict__ exps, uint16_t* __restrict__ out) {
   const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (at >= count) return;                       // count is a multiple of 8
+  if (at >= count) return;                       // count and d are multiples of 8
   float v[4] = {};
   for (int p = 0; p < parts; ++p) {
     const float4 t = *reinterpret_cast<const float4*>(sums + p * count + at);
     v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
   }
-  *reinterpret_cast<uint2*>(out + at) = make_uint2(bf16_bits(v[0]) | static_cast<uint32_t>(bf16_bits(v[1])) << 16,
-                                                   bf16_bits(v[2]) | static_cast<uint32_t>(bf16_bits(v[3])) << 16);
+  const float f = row_factor(targets, weight, inv_tau, static_cast<int>(at / d));
+  const int e = exps->W - 2 * kTop;
+  uint16_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = bf16_bits(__builtin_ldexpf(v[i], e) * f);
+  *reinterpret_cast<uint2*>(out + at) = make_uint2(b[0] | static_cast<uint32_t>(b[1]) << 16, b[2] | static_cast<uint32_t>(b[3]) << 16);
 }
 
 // ---- host --------------------------------------------------------------------------------------------
@@ -381,10 +498,10 @@ hipError_t launch_gemm(GemmArgs a, hipStream_t s) {
 }
 
 hipError_t launch_turn(const uint16_t* from, int64_t ld_from, int rows, int cols, uint16_t* to, int64_t ld_to, int rows_pad,
-                       const int32_t* marks, hipStream_t s) {
+                       const int32_t* marks, const int* exponent, hipStream_t s) {
   if (rows_pad == 0) return hipSuccess;
   hipLaunchKernelGGL(turn_kernel, dim3((rows_pad + kTurn - 1) / kTurn, (cols + kTurn - 1) / kTurn), dim3(256), 0, s, from, ld_from, rows, cols, to,
-                     ld_to, rows_pad, marks);
+                     ld_to, rows_pad, marks, exponent);
   return hipGetLastError();
 }
 
@@ -417,7 +534,7 @@ Plan make_plan(int rows, int n, int d, bool f32) {
   p.dz = up256(2 * rows * p.vpad);
   p.dzt = up256(2 * p.piece * p.mpad * (f32 ? 2 : 1));
   p.sums = p.piece < n || p.parts > 1 ? up256(sizeof(float) * p.parts * static_cast<size_t>(rows) * d) : 0;
-  p.total = p.ht + p.wt + p.dz + p.dzt + p.sums + 256;
+  p.total = p.ht + p.wt + p.dz + p.dzt + p.sums + up256(sizeof(uint3) * kRangeBlocks) + 256;
   return p;
 }
 
@@ -460,8 +577,17 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
   uint16_t* const dz = reinterpret_cast<uint16_t*>(take(p.dz));
   uint16_t* const dzT = reinterpret_cast<uint16_t*>(take(p.dzt));
   float* const sums = p.sums ? reinterpret_cast<float*>(take(p.sums)) : nullptr;
-  hipError_t e = hipSuccess;
-  if (c.dW && (e = launch_turn(c.h, c.d, c.rows, c.d, hT, p.mpad, static_cast<int>(p.mpad), c.targets, s)) != hipSuccess) return e;
+  uint3* const ranges = reinterpret_cast<uint3*>(take(up256(sizeof(uint3) * kRangeBlocks)));
+  Exponents* const exps = reinterpret_cast<Exponents*>(take(256));
+  const int64_t pieces = c.dh ? static_cast<int64_t>(c.n) * c.d / 8 : 0;
+  const int64_t want = (pieces + 256 * 8 - 1) / (256 * 8) > c.rows ? (pieces + 256 * 8 - 1) / (256 * 8) : c.rows;
+  const int blocks = static_cast<int>(want < 1 ? 1 : want < kRangeBlocks ? want : kRangeBlocks);
+  hipLaunchKernelGGL(range_kernel, dim3(blocks), dim3(256), 0, s, reinterpret_cast<const u32x4*>(c.W), pieces,
+                     reinterpret_cast<const u32x4*>(c.h), c.rows, c.d / 8, c.weight, c.targets, ranges);
+  hipLaunchKernelGGL(settle_kernel, dim3(1), dim3(256), 0, s, ranges, blocks, exps);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (c.dW && (e = launch_turn(c.h, c.d, c.rows, c.d, hT, p.mpad, static_cast<int>(p.mpad), c.targets, &exps->h, s)) != hipSuccess) return e;
   const int terms = c.f32 ? 2 : 1;
   for (int v0 = 0; v0 < c.n; v0 += p.piece) {
     const int v = c.n - v0 < p.piece ? c.n - v0 : p.piece;
@@ -473,18 +599,19 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
       a.M = c.rows; a.N = v; a.KT = c.d / 64; a.tail = c.d % 64; a.wrapB = 0x7FFFFFFF; a.KS = 1;
       a.targets = c.targets; a.col0 = v0;
       a.inv_tau = 1.f / c.tau; a.scale2 = kLog2e / c.tau;
-      a.lse = c.lse; a.weight = c.weight;
+      a.lse = c.lse; a.weight = c.weight; a.exps = exps;
       a.dz = c.dh ? dz : nullptr; a.ldz = vpad;
       a.dzT = c.dW ? dzT : nullptr; a.ldT = p.mpad * terms; a.lo = static_cast<int>(p.mpad); a.two_terms = c.f32;
       if ((e = launch_gemm<kGradient>(a, s)) != hipSuccess) return e;
     }
     if (c.dh && c.rows > 0) {
-      if ((e = launch_turn(W, c.d, v, c.d, WT, vpad, static_cast<int>(vpad), nullptr, s)) != hipSuccess) return e;
+      if ((e = launch_turn(W, c.d, v, c.d, WT, vpad, static_cast<int>(vpad), nullptr, &exps->W, s)) != hipSuccess) return e;
       GemmArgs a{};
       a.A = dz; a.B = WT; a.lda = a.ldb = vpad;
       a.M = c.rows; a.N = c.d; a.KT = static_cast<int>(vpad / 64); a.wrapB = 0x7FFFFFFF; a.KS = p.parts;
       a.sums = sums; a.first = v0 == 0; a.last = p.parts == 1 && v0 + v == c.n;
       a.out = c.dh;
+      a.targets = c.targets; a.weight = c.weight; a.inv_tau = 1.f / c.tau; a.exps = exps;
       if ((e = launch_gemm<kRows>(a, s)) != hipSuccess) return e;
     }
     if (c.dW) {
@@ -495,12 +622,14 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
       a.out = c.f32 ? static_cast<void*>(static_cast<float*>(c.dW) + static_cast<int64_t>(v0) * c.d)
                     : static_cast<void*>(static_cast<uint16_t*>(c.dW) + static_cast<int64_t>(v0) * c.d);
       a.f32 = c.f32; a.accumulate = c.accumulate;
+      a.inv_tau = 1.f / c.tau; a.exps = exps;
       if ((e = launch_gemm<kTable>(a, s)) != hipSuccess) return e;
     }
   }
   if (c.dh && c.rows > 0 && p.parts > 1) {
     const int64_t count = static_cast<int64_t>(c.rows) * c.d;
-    hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((count / 4 + 255) / 256)), dim3(256), 0, s, sums, p.parts, count, c.dh);
+    hipLaunchKernelGGL(join_rows_kernel, dim3(static_cast<uint32_t>((count / 4 + 255) / 256)), dim3(256), 0, s, sums, p.parts, count, c.d,
+                       c.targets, c.weight, 1.f / c.tau, exps, c.dh);
     e = hipGetLastError();
   }
   return e;

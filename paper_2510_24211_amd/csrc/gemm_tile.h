@@ -1,5 +1,5 @@
 // A workgroup's tile of a matrix product whose operands both have k along their rows:
-//   acc[a, b] = sum_k A[a, k] * B[b, k]        bf16 x bf16 -> fp32 (MFMA)
+//   acc[a, b] = sum_k A[a, k] * B[b, k]        bf16 x bf16 or fp16 x fp16 -> fp32 (MFMA)
 // HR rows of A x BN rows of B by eight wavefronts, k in tiles of 64, staged in LDS by loads that name no register.
 #pragma once
 #include "tile_loads.h"
@@ -41,7 +41,7 @@ struct TileOperand {
 //   * Loads are issued one by one between MFMAs: eight wavefronts issuing all of theirs after the barrier would queue at
 //     the one address unit with their MFMAs behind them.
 // Ends with loads, MFMAs' operands and stages all settled for this wavefront; a barrier has to follow before LDS is reused.
-template <class K>
+template <class K, bool F16>
 __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const TileOperand& A, const TileOperand& B, const int kt0,
                                               const int KT, const int tail, const int rot, f32x16 (&acc)[K::NC][K::NB]) {
   constexpr int NC = K::NC, NB = K::NB, AL = K::AL, BL = K::BL, SA = K::SA, SB = K::SB;
@@ -112,8 +112,12 @@ __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const Ti
     constexpr int P0 = Q < 4 ? NP * Q / 4 : 0, P1 = Q < 4 ? NP * (Q + 1) / 4 : 0;
     static_for<NM>([&](auto ii) {
       constexpr int I = decltype(ii)::value, c = I / NB, i = I % NB;
-      acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, aq[q][i]),
-                                                          __builtin_bit_cast(bf16x8, bq[q][c]), acc[c][i], 0, 0, 0);
+      if constexpr (F16)
+        acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, aq[q][i]), __builtin_bit_cast(f16x8, bq[q][c]),
+                                                           acc[c][i], 0, 0, 0);
+      else
+        acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, aq[q][i]), __builtin_bit_cast(bf16x8, bq[q][c]),
+                                                            acc[c][i], 0, 0, 0);
       constexpr int F = P0 + (P1 - P0) * I / NM, E = P0 + (P1 - P0) * (I + 1) / NM;
       if constexpr (E > F) {
         __builtin_amdgcn_sched_barrier(0);

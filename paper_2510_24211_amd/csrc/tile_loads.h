@@ -10,6 +10,7 @@ namespace scd {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 // 16-byte register value; a native vector (the HIP struct type is copied with memcpy,
 // which keeps arrays of it in scratch memory)

@@ -5,8 +5,9 @@ errors of one chain are independent, so sqrt(d) of them with a margin of 4 is ta
 matrix unit makes at once count as one).  With E the largest error of a row's logits, lse errs by at most E and by its own
 arithmetic: exponentials and logarithms of 2 to 1 ulp of arguments up to |z| log2(e), a sum of n positive terms added up in a
 tree: 16 u (1 + |z|max).  loss = lse - z_t errs by twice that.
-dz errs by the relative error of p, e_p = 2 E + 16 u (1 + |z|max), and by its rounding to bf16, 2^-8 (2^-16 in two terms); the
-products add the same kind of chain; the result is rounded to its type.  The roundings of dz's terms are taken at their
+dz errs by the relative error of p, e_p = 2 E + 16 u (1 + |z|max), and by its rounding to fp16, 2^-11 (2^-22 in two terms) of
+itself and 2^-25 units in the place of 2^-14 (2^-39) of the largest weight; h and W may err by 2^-39 of their largest element,
+to which that of dz, at most 1, adds nothing that its own 2^-39 does not cover; the products add the same kind of chain; the result is rounded to its type.  The roundings of dz's terms are taken at their
 full size and of one sign: sum |dz| |W|.
 Underflow: fp32 and bf16 hold nothing between 0 and 2^-126 but denormal numbers, which the units may take for 0.  p is off by up
 to 2^-126 more for that, and so is each of dz's terms (a rest that its first term leaves may be that small where dz itself is
@@ -57,13 +58,15 @@ def _oracle(h, W, t, w, tau, two_terms=False):
     coef = torch.where(there, w.double() / tau, 0.0)[:, None]
     dz = coef * (p - hot)
     e_dz = coef.abs() * p * (2 * E + 32 * U * (1 + zmax))[:, None]
-    bf, tab = 2.0 ** -8, (2.0 ** -16 if two_terms else 2.0 ** -8)
+    bf, tab = 2.0 ** -11, (2.0 ** -22 if two_terms else 2.0 ** -11)
+    w_max = w[there].abs().max().double() if there.any() else 1.0
+    floor = 2.0 ** -38 * w_max / tau
     r = dict(loss=loss, lse=lse, dh=dz @ W, dW=dz.t() @ h)
     tiny = 3 * 2.0 ** -126
     chain_n, chain_m = 4 * math.sqrt(n) * U, 4 * math.sqrt(max(h.shape[0], 1)) * U
     b = dict(loss=2 * e_lse + 4 * U * (lse.abs() + zt.abs()), lse=e_lse + 4 * U * lse.abs(),
-             dh=(e_dz + dz.abs() * (bf + chain_n + 4 * U) + tiny) @ W.abs() + tiny,
-             dW=(e_dz + dz.abs() * (tab + chain_m + 4 * U) + tiny).t() @ h.abs() + tiny)
+             dh=(e_dz + dz.abs() * (bf + chain_n + 4 * U) + tiny + coef.abs() * 2.0 ** -38) @ W.abs() + tiny,
+             dW=(e_dz + dz.abs() * (tab + chain_m + 4 * U) + tiny + floor).t() @ h.abs() + tiny)
     return r, b
 
 
