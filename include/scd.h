@@ -275,6 +275,36 @@ int scd_lm_head_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
  * (d_z fp32 [B, L, n], window order) instead of computed by the LM head. */
 int scd_step_logits(scd_ctx* ctx, const float* d_z, void* d_state);
 
+/* ---- the LM head over 4-bit weights -----------------------------------------------------------
+ *   W[v, k] = s[v, k / group] * (q[v, k] - o[v, k / group]),   q in 0..15, o = 8, or a zero point of 0..15.
+ * group: weights of a row that share a scale, a positive multiple of 32 (the last group of a row may be shorter), at most 256
+ * groups per row.  Row-major arrays, as a checkpoint holds them: d_codes uint8 [V, d / 2], even k in the low half of a
+ * byte (4-byte aligned); d_scales bf16 [V, G] and d_zeros uint8 [V, G] (NULL: o = 8), G = ceil(d / group).  The steps read
+ * them in another layout, made once by scd_pack_quantized.  All need cfg.d > 0. */
+typedef struct scd_quantized {
+  const void* d_packed;   /* written by scd_pack_quantized for this configuration's allowed ids and d */
+  int32_t group;
+  int32_t zeros;          /* 1: with zero points, 0: without                                           */
+} scd_quantized;
+
+/* Bytes of the layout; 0 on a bad configuration or group. */
+size_t scd_quantized_bytes(const scd_config* cfg, int32_t group, int32_t zeros);
+
+/* Quantises W bf16 [V, d] (finite): codes and scales, and zero points unless d_zeros is NULL.  Without them s = max(largest / 7,
+ * -smallest / 8) of a group, with them s = (largest - smallest) / 15 over a range that holds 0, rounded to bf16; the
+ * codes are the nearest. */
+int scd_quantize(scd_ctx* ctx, const uint16_t* d_W, int32_t group, uint8_t* d_codes, uint16_t* d_scales, uint8_t* d_zeros);
+
+/* Lays the allowed rows out: d_packed, scd_quantized_bytes(cfg, group, d_zeros != NULL) bytes, 256-byte aligned.  Zero points above 15
+ * count as 15. */
+int scd_pack_quantized(scd_ctx* ctx, const uint8_t* d_codes, const uint16_t* d_scales, const uint8_t* d_zeros, int32_t group,
+                       void* d_packed);
+
+/* scd_lm_head and scd_step with these weights in the place of W.  The products are exact and summed in fp32: no weight is
+ * rounded to bf16. */
+int scd_lm_head_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, float* d_z);
+int scd_step_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, void* d_state);
+
 /* ---- the vocabulary table at the model's other end, and what it learns -------------------------
  * The same table W, bf16 bits [V, d] row-major, all pointers 16-byte aligned (d_ids, d_targets and the
  * float arrays 4-byte).  All of them need cfg.d > 0; of the rest of the configuration they use what is

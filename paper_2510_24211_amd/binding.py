@@ -42,6 +42,10 @@ class ScdConfig(ctypes.Structure):
                 ("seed", ctypes.c_uint64)]
 
 
+class ScdQuantized(ctypes.Structure):
+    _fields_ = [("d_packed", ctypes.c_void_p), ("group", ctypes.c_int32), ("zeros", ctypes.c_int32)]
+
+
 class ScdError(RuntimeError):
     def __init__(self, code, what):
         super().__init__(f"{what}: {code} ({strerror(code)})")
@@ -81,6 +85,13 @@ def load():
     lib.scd_set_lm_head_events.argtypes = [vp, vp, vp]
     lib.scd_lm_head_kernel_name.argtypes = [vp, ctypes.c_char_p, sz]
     f32 = ctypes.c_float
+    quantp = ctypes.POINTER(ScdQuantized)
+    lib.scd_quantized_bytes.restype = sz
+    lib.scd_quantized_bytes.argtypes = [cfgp, i32, i32]
+    lib.scd_quantize.argtypes = [vp, vp, i32, vp, vp, vp]
+    lib.scd_pack_quantized.argtypes = [vp, vp, vp, vp, i32, vp]
+    lib.scd_lm_head_quantized.argtypes = [vp, vp, quantp, vp]
+    lib.scd_step_quantized.argtypes = [vp, vp, quantp, vp]
     lib.scd_embed.argtypes = [vp, vp, i32, vp, f32, vp]
     lib.scd_embed_window.argtypes = [vp, vp, vp, f32, vp]
     lib.scd_embed_backward_workspace_bytes.restype = sz
@@ -99,7 +110,8 @@ def load():
     lib.scdw_copy.argtypes = [vp, vp, vp, sz]
     for name in ("scd_create", "scd_destroy", "scd_reset", "scd_state_field", "scd_lm_head",
                  "scd_select", "scd_couple_draft", "scd_couple_draft_static", "scd_verify", "scd_step", "scd_step_logits",
-                 "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_embed", "scd_embed_window",
+                 "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_quantize",
+                 "scd_pack_quantized", "scd_lm_head_quantized", "scd_step_quantized", "scd_embed", "scd_embed_window",
                  "scd_embed_backward", "scd_cross_entropy", "scd_cross_entropy_backward",
                  "scd_status", "scdw_gather_hidden", "scdw_copy"):
         getattr(lib, name).restype = ctypes.c_int
@@ -149,6 +161,13 @@ def _grad_type(dtype):
     if dtype not in _GRAD:
         raise TypeError(f"gradient of W: dtype {dtype}, expected one of {tuple(_GRAD)}")
     return _GRAD[dtype]
+
+
+class QuantizedWeights:
+    """4-bit weights as pack_quantized lays them out for one configuration."""
+
+    def __init__(self, data, group, zeros):
+        self.data, self.group, self.zeros = data, group, zeros
 
 
 class Scd:
@@ -275,6 +294,43 @@ class Scd:
         self._check(self.lib.scd_step_logits(
             self.ctx, _ptr(z, (torch.float32,), c.B * c.L * self.n, "z"),
             _ptr(state, (torch.uint8,), state_bytes(c), "state")), "scd_step_logits")
+
+    # -- 4-bit weights ----------------------------------------------------------
+    def quantize(self, W, group, codes, scales, zeros=None):
+        c = self.cfg
+        G = -(-c.d // group) if group > 0 else 0
+        self._check(self.lib.scd_quantize(
+            self.ctx, _ptr(W, _BF16, c.V * c.d, "W"), int(group), _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"),
+            _ptr(scales, _BF16, c.V * G, "scales"), _ptr(zeros, (torch.uint8,), c.V * G, "zeros")), "scd_quantize")
+
+    def pack_quantized(self, codes, scales, zeros, group):
+        """The weights in the layout that lm_head_quantized and step_quantized read, in memory of their own."""
+        c = self.cfg
+        need = self.lib.scd_quantized_bytes(ctypes.byref(c), int(group), int(zeros is not None))
+        G = -(-c.d // group) if need else 0
+        packed = QuantizedWeights(self._workspace(need, "scd_quantized_bytes"), int(group), zeros is not None)
+        self._check(self.lib.scd_pack_quantized(
+            self.ctx, _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"), _ptr(scales, _BF16, c.V * G, "scales"),
+            _ptr(zeros, (torch.uint8,), c.V * G, "zeros"), int(group), ctypes.c_void_p(packed.data.data_ptr())), "scd_pack_quantized")
+        return packed
+
+    def _quantized(self, W):
+        need = self.lib.scd_quantized_bytes(ctypes.byref(self.cfg), W.group, int(W.zeros))
+        if need == 0:
+            raise ScdError(SCD_EINVAL, "scd_quantized_bytes")
+        return ctypes.byref(ScdQuantized(_ptr(W.data, (torch.uint8,), need, "quantized weights"), W.group, int(W.zeros)))
+
+    def lm_head_quantized(self, h, W, z):
+        c = self.cfg
+        self._check(self.lib.scd_lm_head_quantized(
+            self.ctx, _ptr(h, _BF16, c.B * self.C * c.L * c.d, "h"), self._quantized(W),
+            _ptr(z, (torch.float32,), c.B * c.L * self.n, "z")), "scd_lm_head_quantized")
+
+    def step_quantized(self, h, W, state):
+        c = self.cfg
+        self._check(self.lib.scd_step_quantized(
+            self.ctx, _ptr(h, _BF16, c.B * self.C * c.L * c.d, "h"), self._quantized(W),
+            _ptr(state, (torch.uint8,), state_bytes(c), "state")), "scd_step_quantized")
 
     # -- the vocabulary table at the model's other end, and what it learns ----------
     def _workspace(self, need, what):

@@ -356,6 +356,20 @@ int couple_draft_impl(scd_ctx* c, char* w, bool cands, const float* d_z_cur, con
   return hip_rc(scd::launch_row(ra, c->stream, c->row_lds));
 }
 
+bool valid_group(const scd_config& c, int32_t group) {
+  return c.d > 0 && group > 0 && group % 32 == 0 && (static_cast<int64_t>(c.d) + group - 1) / group <= scd::kMaxGroups;
+}
+int quantized_args(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, scd::LmHeadArgs* a) {
+  if (!c || !d_h || !W || !W->d_packed || !aligned(d_h, 16) || !aligned(W->d_packed, kAlign)) return SCD_EINVAL;
+  if (!valid_group(c->cfg, W->group) || (W->zeros != 0 && W->zeros != 1)) return SCD_EINVAL;
+  a->h = d_h;
+  a->B = c->cfg.B; a->C = c->C; a->L = c->cfg.L; a->N = c->cfg.N; a->d = c->cfg.d; a->n = c->n;
+  a->lam = c->cfg.cfg_lambda;
+  a->one_plus_lam = 1.0f + c->cfg.cfg_lambda;
+  a->tau = c->cfg.temperature;
+  return SCD_OK;
+}
+
 // What the operators on the vocabulary table check alike.
 constexpr int32_t kCrossEntropyRows = 1 << 20;
 inline bool valid_gradient(int32_t grad_type, int32_t accumulate) {
@@ -489,6 +503,48 @@ int scd_lm_head_kernel_name(scd_ctx* c, char* host_buf, size_t cap) {
 int scd_step_logits(scd_ctx* c, const float* d_z, void* st) {
   if (!c || !d_z || !st || !aligned(st, kAlign)) return SCD_EINVAL;
   return run_tail(c, st, 0, d_z);
+}
+
+// ---- the LM head over 4-bit weights ----------------------------------------------------------
+size_t scd_quantized_bytes(const scd_config* cfg, int32_t group, int32_t zeros) {
+  if (!valid_config(cfg) || !valid_group(*cfg, group) || (zeros != 0 && zeros != 1)) return 0;
+  return scd::quantized_bytes(cfg->v_hi - cfg->v_lo, cfg->d, group, zeros != 0);
+}
+
+int scd_quantize(scd_ctx* c, const uint16_t* d_W, int32_t group, uint8_t* d_codes, uint16_t* d_scales, uint8_t* d_zeros) {
+  if (!c || !d_W || !d_codes || !d_scales || !valid_group(c->cfg, group)) return SCD_EINVAL;
+  if (!aligned(d_W, 16) || !aligned(d_codes, 4) || !aligned(d_scales, 2)) return SCD_EINVAL;
+  return hip_rc(scd::launch_quantize(d_W, c->cfg.V, c->cfg.d, group, d_codes, d_scales, d_zeros, c->stream));
+}
+
+int scd_pack_quantized(scd_ctx* c, const uint8_t* d_codes, const uint16_t* d_scales, const uint8_t* d_zeros, int32_t group,
+                       void* d_packed) {
+  if (!c || !d_codes || !d_scales || !d_packed || !valid_group(c->cfg, group)) return SCD_EINVAL;
+  if (!aligned(d_codes, 4) || !aligned(d_scales, 2) || !aligned(d_packed, kAlign)) return SCD_EINVAL;
+  const int groups = (c->cfg.d + group - 1) / group;
+  const size_t row = c->cfg.v_lo;
+  return hip_rc(scd::launch_pack_quantized(d_codes + row * (c->cfg.d / 2), d_scales + row * groups, d_zeros ? d_zeros + row * groups : nullptr,
+                                           c->n, c->cfg.d, group, d_packed, c->stream));
+}
+
+int scd_lm_head_quantized(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, float* d_z) {
+  scd::LmHeadArgs a{};
+  if (!d_z || !aligned(d_z, 4)) return SCD_EINVAL;
+  if (int rc = quantized_args(c, d_h, W, &a); rc != SCD_OK) return rc;
+  a.z = d_z;
+  return hip_rc(scd::launch_lm_head_quantized(a, W->d_packed, W->group, W->zeros != 0, c->stream));
+}
+
+int scd_step_quantized(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, void* st) {
+  scd::LmHeadArgs a{};
+  if (!st || !aligned(st, kAlign)) return SCD_EINVAL;
+  if (int rc = quantized_args(c, d_h, W, &a); rc != SCD_OK) return rc;
+  a.z = field<float>(c, st, SCD_F_Z);
+  a.pos = field<int32_t>(c, st, SCD_F_POS);
+  a.iter = field<int32_t>(c, st, SCD_F_ITER);
+  a.parity_stride = static_cast<size_t>(c->cfg.B) * c->cfg.L * c->n;
+  if (scd::launch_lm_head_quantized(a, W->d_packed, W->group, W->zeros != 0, c->stream) != hipSuccess) return SCD_EHIP;
+  return run_tail(c, st, 0, nullptr);
 }
 
 // ---- operators on the vocabulary table ---------------------------------------------------

@@ -215,4 +215,18 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t s);
 size_t cross_entropy_backward_bytes(int rows, int n, int d, bool f32);
 hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& a, hipStream_t s);
 
+// The LM head over 4-bit weights, laid out by launch_pack_quantized.  Of LmHeadArgs it reads what z and the rows of h need.
+struct QuantizedArgs {
+  const void* codes;
+  const void* scales;
+  int group, groups;    // weights of a row that share a scale (a multiple of 32), and how many such groups a row has
+  bool zeros;           // scales come with zero points
+};
+constexpr int kMaxGroups = 256;
+size_t quantized_bytes(int n, int d, int group, bool zeros);
+hipError_t launch_quantize(const uint16_t* W, int V, int d, int group, uint8_t* codes, uint16_t* scales, uint8_t* zeros, hipStream_t s);
+hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, int d, int group, void* packed,
+                                 hipStream_t s);
+hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s);
+
 }  // namespace scd
