@@ -4,17 +4,19 @@
 //
 // A code becomes the bf16 number 16 + q by one shift and one bitwise operation for two of them (q is put behind the leading
 // mantissa bit), so the products go to the matrix units exactly:
-//   sum over a group of h * (q - o) = sum h * (16 + q) - (16 + o) * sum h,
-// the second sum by a product of the same rows with ones.  At a group's end both are scaled and added to the
-// fp32 logits: no weight is ever rounded.
+//   sum over a group of h * (q - o) = sum h * (16 + q) - (16 + o) * sum h.
+// The second sum is taken once per workgroup, by whoever loaded the rows.  It goes to the matrix units too, split into three
+// bf16 terms of 8 bits each that hold all 24, times -(16 + o), which bf16 holds: one more MFMA for each four (C operands of that
+// value would cost four times the LDS reads).  At a group's end the accumulators are scaled and added to the fp32 logits: no
+// weight is ever rounded.
 //
 // Layout.  Columns in tiles of 32, k in blocks of 64: a block of a tile is 1 KB, 16 bytes for each lane of a wavefront, which
 // are its operands of four 32x32x16 MFMAs (lane l: column l % 32; word j: k = 16 j + 8 (l / 32) + 0 .. 7, even k in
 // the low half, odd k in the high half of the word).  The blocks of a tile follow each other; behind all of them, per tile
 // and group, the 32 columns' scales (2 bytes each; with zero points 4, the second two holding 16 + o as bf16).
 //
-// A workgroup of NW wavefronts owns NW / WK neighbouring column tiles; WK wavefronts share a tile and take 1/WK of k each
-// (their sums are added up at the end in a fixed order).  Weights and h rows go from memory straight into
+// A workgroup of NW wavefronts owns NC * NW / WK neighbouring column tiles, NC per wavefront; WK wavefronts share tiles and take
+// 1/WK of k each (their sums are added up at the end in a fixed order).  Weights and h rows go from memory straight into
 // LDS, S stages deep; a wavefront reads its own weights back, the h rows are shared.  The scales of the workgroup's columns are
 // fetched whole at the start.
 #include "lm_head_rows.h"
@@ -24,23 +26,23 @@ namespace scd {
 namespace {
 
 constexpr int kTileCols = 32, kBlockK = 64, kBlockBytes = 1024, kTilesPad = 8;
-constexpr int kLdsBytes = 160 * 1024;
 
-// rows per block of 32 that are really loaded: HRB; blocks per workgroup (guidance included): NB
-template <int C_, int RB_, int HRB_, int NW_, int WK_>
+// rows per block of 32 that are really loaded: HRB; blocks per workgroup (guidance included): NB; KB of LDS it may take: KB
+template <int C_, int RB_, int HRB_, int NC_, int NW_, int WK_, int KB_>
 struct QuantCfg {
-  static constexpr int C = C_, RB = RB_, HRB = HRB_, NW = NW_, WK = WK_;
-  static constexpr int THREADS = NW * 64, WC = NW / WK, NB = RB * C;
+  static constexpr int C = C_, RB = RB_, HRB = HRB_, NC = NC_, NW = NW_, WK = WK_, LDS = KB_ * 1024;
+  static constexpr int THREADS = NW * 64, WC = NW / WK, COLTILES = WC * NC, NB = RB * C;
   static constexpr int HROWS = NB * HRB;                 // h rows per part of k
   static constexpr int HI = WK * HROWS / 8;              // load instructions for the h rows of a step, all parts
   static constexpr int HL = (HI + NW - 1) / NW;          // per wavefront
-  static constexpr int WB = NW * kBlockBytes, HB = WK * HROWS * 128, STAGE = WB + HB;
-  static constexpr int S = 120 * 1024 / STAGE < 2 ? 2 : 120 * 1024 / STAGE > 6 ? 6 : 120 * 1024 / STAGE;
-  static constexpr int RED = WK > 1 ? NW * NB * 16 * 64 * 4 : 0;      // sums of the parts of k, in the place of the stages
+  static constexpr int WB = NW * NC * kBlockBytes, HB = WK * HROWS * 128, STAGE = WB + HB;
+  static constexpr int FIT = (LDS - LDS / 6) / STAGE, S = FIT > 7 ? 7 : FIT;
+  static constexpr int RED = WK > 1 ? NW * NC * NB * 16 * 64 * 4 : 0;      // sums of the parts of k, in the place of the stages
   static constexpr int BASE = S * STAGE > RED ? S * STAGE : RED;
   static constexpr int TABLE = RB * 32 * 4;
-  static constexpr int SCALES = kLdsBytes - TABLE - BASE;      // room for the columns' scales
-  static_assert(SCALES >= WC * 4 * 1024, "LDS");
+  static constexpr int SUMS = 2 * WK * 2 * HROWS * 8;    // rows' sums of two steps, of the halves of a block
+  static constexpr int SCALES = LDS - TABLE - SUMS - BASE;          // room for the columns' scales
+  static_assert(S >= 3 && SCALES >= COLTILES * 1024, "LDS");
 };
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
@@ -48,17 +50,18 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
 }
 // the eight codes of a word as bf16 numbers 16 + q
 __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t w) {
-  constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-  return u32x4{(w << 3 & kMask) | kSixteen, (w >> 1 & kMask) | kSixteen, (w >> 5 & kMask) | kSixteen, (w >> 9 & kMask) | kSixteen};
+  auto two = [](uint32_t x) -> uint32_t { return __builtin_amdgcn_bitop3_b32(x, 0x00780078u, 0x41804180u, 0xEA); };      // (x & mask) | sixteen
+  return u32x4{two(w << 3), two(w >> 1), two(w >> 5), two(w >> 9)};
 }
 
 // STEP: MFMAs between two applications of a scale (2: groups that end inside a block of k, 4: they do not)
-template <class K, int STEP>
+template <class K, int STEP, bool ZEROS>
 __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmHeadArgs a, const QuantizedArgs q, const int WT, const int MT) {
-  constexpr int C = K::C, RB = K::RB, NB = K::NB, WK = K::WK, WC = K::WC, NW = K::NW, S = K::S, HL = K::HL, HRB = K::HRB;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kLdsBytes];
+  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, WK = K::WK, WC = K::WC, NW = K::NW, S = K::S, HL = K::HL, HRB = K::HRB;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[K::LDS];
   int* const table = reinterpret_cast<int*>(lds + K::BASE);
-  unsigned char* const slab = lds + K::BASE + K::TABLE;
+  uint2* const hsum = reinterpret_cast<uint2*>(lds + K::BASE + K::TABLE);     // [2][WK][2][HROWS]
+  unsigned char* const slab = lds + K::BASE + K::TABLE + K::SUMS;
   // workgroups that share columns get ids 8 apart: the same XCD, the same L2
   const int id = blockIdx.x, mt = (id / 8) % MT, wt = id / (8 * MT) * 8 + id % 8;
   if (wt >= WT) return;
@@ -66,7 +69,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wc = wave % WC, part = wave / WC;
   const int rows = a.B * a.L, p_base = mt * RB * 32, d = a.d;
-  const int tile = wt * WC + wc;                         // column tile (the layout is padded to whole workgroups)
+  const int tile = (wt * WC + wc) * NC;                  // first column tile (the layout is padded to whole workgroups)
   const int KB = (d + kBlockK - 1) / kBlockK;
   const int nch = d % kBlockK / 8;                       // 16-byte chunks of a ragged last block, 0: there is none
   auto first_block = [&](int p) { return KB * p / WK; };
@@ -76,12 +79,13 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds));
   // ---- scales of the workgroup's columns ---------------------------------------------------------------
-  const int esize = q.zeros ? 4 : 2, tile_scales = q.groups * kTileCols * esize;
+  constexpr int esize = ZEROS ? 4 : 2;
+  const int tile_scales = q.groups * kTileCols * esize;
   {
-    const uint64_t from = reinterpret_cast<uint64_t>(q.scales) + static_cast<uint64_t>(wt) * WC * tile_scales;
-    const int pieces = (WC * tile_scales + 1023) / 1024;
+    const uint64_t from = reinterpret_cast<uint64_t>(q.scales) + static_cast<uint64_t>(wt) * K::COLTILES * tile_scales;
+    const int pieces = (K::COLTILES * tile_scales + 1023) / 1024;
     for (int i = wave; i < pieces; i += NW)
-      load_lds16<false, 0>(from + static_cast<uint64_t>(i) * 1024, lane * 16, lds0 + K::BASE + K::TABLE + i * 1024);
+      load_lds16<false, 0>(from + static_cast<uint64_t>(i) * 1024, lane * 16, lds0 + K::BASE + K::TABLE + K::SUMS + i * 1024);
   }
   // ---- loads of a step: this wavefront's block of weights, its share of the h rows ---------------------------
   const uint64_t wbase = reinterpret_cast<uint64_t>(q.codes) + static_cast<uint64_t>(tile) * KB * kBlockBytes;
@@ -99,130 +103,273 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
               static_cast<uint32_t>(d) * 2u;
     hlds[i] = lds0 + K::WB + piece * 1024;
   }
-  auto block_of = [&](int p, int t) {                    // block of k that part p works on in step t
-    const int b0 = first_block(p), n = first_block(p + 1) - b0;
-    return min(b0 + min(t, max(n - 1, 0)), KB - 1);
-  };
-  auto load = [&](int t, int stage) {
+  // Every part walks its blocks cyclically from a start of the workgroup's own: rows of h are d * 2 bytes apart, and from one
+  // start all of the chip would ask for the same address bits at the same time.  `at`: the block's index in its part; a part may
+  // have one block less than T, and loads some other in its place.
+  const int rot = wt * 5 % T;
+  auto next_of = [&](int at) { return at + 1 == T ? 0 : at + 1; };
+  int hfirst[HL];
+#pragma unroll
+  for (int i = 0; i < HL; ++i) hfirst[i] = first_block(hpart[i]);
+  auto load_h = [&](int at, int stage) __attribute__((always_inline)) {
     static_for<HL>([&](auto ii) {
       constexpr int i = decltype(ii)::value;
-      const int kb = block_of(hpart[i], t);
-      const int chunk = nch && kb == KB - 1 ? min(hchunk[i], nch - 1) : hchunk[i];
-      load_lds16<false, 0>(hbase + static_cast<uint32_t>(kb) * 128u, hoff[i] + chunk * 16, hlds[i] + stage * K::STAGE);
+      const int kb = __builtin_amdgcn_readfirstlane(min(hfirst[i] + at, KB - 1));
+      uint32_t off = hoff[i] + hchunk[i] * 16;
+      if (nch && kb == KB - 1) off = hoff[i] + min(hchunk[i], nch - 1) * 16;
+      load_lds16<false, 0>(hbase + static_cast<uint32_t>(kb) * 128u, off, __builtin_amdgcn_readfirstlane(hlds[i]) + stage * K::STAGE);
     });
-    load_lds16<false, 0>(wbase + static_cast<uint64_t>(block_of(part, t)) * kBlockBytes, lane * 16, lds0 + wave * 1024 + stage * K::STAGE);
+  };
+  auto load_w = [&](int at, int stage) __attribute__((always_inline)) {
+    const uint64_t from = wbase + static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(min(kb0 + at, KB - 1))) * static_cast<uint64_t>(kBlockBytes);
+    static_for<NC>([&](auto c) {
+      constexpr int i = decltype(c)::value;
+      load_lds16<false, i * 1024>(from + static_cast<uint64_t>(i) * KB * kBlockBytes, lane * 16, lds0 + wave * (NC * 1024) + stage * K::STAGE);
+    });
   };
   // the ragged block: chunks past the end are zeroed by the wavefront that loaded something in their place
-  auto clear_ragged = [&](int t, int stage) {
+  auto clear_ragged = [&](int at, int stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < HL; ++i)
-      if (block_of(hpart[i], t) == KB - 1 && hchunk[i] >= nch)
+      if (hfirst[i] + at >= KB - 1 && hchunk[i] >= nch)
         *reinterpret_cast<u32x4*>(lds + (hlds[i] - lds0) + stage * K::STAGE + lane * 16) = u32x4{0u, 0u, 0u, 0u};
   };
 
-  f32x16 sum[NB];
+  // Sums of the h rows that this wavefront loaded: 8 lanes hold a row's block of k, 4 a half.
+  auto add_rows = [&](int parity, int stage) __attribute__((always_inline)) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
 #pragma unroll
-  for (int i = 0; i < NB; ++i) sum[i] = f32x16{};
-  const int per_group = q.group / 32;                    // half blocks of k
-  auto compute = [&](int kb, int stage) {
-    const unsigned char* const Ht = lds + stage * K::STAGE + K::WB + part * (K::HROWS * 128);
-    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + stage * K::STAGE + wave * 1024 + lane * 16);
-    const u32x4 ones{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-    u32x4 h[4][NB];
+    for (int i = 0; i < HL; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (hlds[i] - lds0) + stage * K::STAGE + lane * 16);
+      float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int r = i * HRB + ln % HRB;
-        h[j][i] = *reinterpret_cast<const u32x4*>(Ht + r * 128 + (((2 * j + lg) ^ ((r >> 1) & 7)) * 16));
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = v[e];           // (a bit cast of the element itself takes the vector's first)
+        s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, s, false);
       }
-#pragma unroll
-    for (int j0 = 0; j0 < 4; j0 += STEP) {
-      const int g = static_cast<int>(static_cast<uint32_t>(kb * 2 + j0 / 2) / static_cast<uint32_t>(per_group));
-      const unsigned char* const at = slab + (wc * q.groups + g) * (kTileCols * esize) + ln * esize;
-      float s, o;
-      if (q.zeros) {
-        const uint32_t both = *reinterpret_cast<const uint32_t*>(at);
-        s = __uint_as_float(both << 16);
-        o = __uint_as_float(both & 0xFFFF0000u);
+      // chunk c of the row sits in slot c ^ swizzle: the lanes of a half are those whose slots differ in the low two bits
+      s += dpp_f32<kDppXor1>(s);
+      s += dpp_f32<kDppXor2>(s);
+      if (STEP == 4) s += dpp_f32<kDppHalfMirror>(s);
+      const uint32_t first = __float_as_uint(s) & 0xFFFF0000u;
+      const float r1 = s - __uint_as_float(first);
+      const uint32_t second = __float_as_uint(r1) & 0xFFFF0000u;
+      const float r2 = r1 - __uint_as_float(second);
+      const int r = (hlds[i] - lds0 - K::WB) / 128 % K::HROWS + (lane >> 3);
+      uint2* const to = hsum + (parity * WK + hpart[i]) * 2 * K::HROWS + r;
+      const uint2 terms = make_uint2(first >> 16 | second, __float_as_uint(r2) >> 16);
+      if (STEP == 4) {
+        if ((lane & 7) == 0) to[0] = terms;
       } else {
-        s = __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at)) << 16);
-        o = 24.f;
+        if ((lane & 3) == 0) to[(hchunk[i] >> 2) * K::HROWS] = terms;
       }
-      f32x16 acc[NB], all[NB];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) acc[i] = all[i] = f32x16{};
-#pragma unroll
-      for (int j = j0; j < j0 + STEP; ++j) {
-        const u32x4 b = codes_to_bf16(w[j]);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) acc[i] = mfma(h[j][i], b, acc[i]);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) all[i] = mfma(h[j][i], ones, all[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum[i][e] = __builtin_fmaf(s, __builtin_fmaf(-o, all[i][e], acc[i][e]), sum[i][e]);
     }
   };
 
-  // Step t: its loads are there (S - 2 steps' are still on their way), the barrier publishes them and says that every
-  // wavefront is done with the stage of step t - 1, which takes the loads of step t + S - 1.
-  constexpr int LPT = HL + 1;
+  // What a step starts with, in registers: the weights' codes, the h rows' operands of the first half and, per half block with
+  // STEP = 2, the terms of this lane's rows' sums and the scales (and zero points).
+  constexpr int PER = 4 / STEP;
+  struct Operands {
+    u32x4 w[NC], h[2][NB];
+    uint2 rows[PER][NB];
+    uint32_t scale[PER][NC];
+  };
+  const int per_group = q.group / 32;                    // half blocks of k
+  int g = 0, left = 0;                                   // group of the next half block; of it, left
+  auto group_at = [&](int kb) __attribute__((always_inline)) {
+    g = kb * 2 / per_group;
+    left = per_group - kb * 2 % per_group;
+  };
+  const unsigned char* const hrows = lds + K::WB + part * (K::HROWS * 128) + ln % HRB * 128;
+  const unsigned char* const scales = slab + wc * NC * q.groups * (kTileCols * esize) + ln * esize;
+  uint32_t hslot[4];                                     // of the first block's rows; rows 8 apart differ in bit 2 of the swizzle
 #pragma unroll
-  for (int t = 0; t < S - 1; ++t)
-    if (t < T) load(t, t);
-  int stage = 0, next = S - 1;
-#pragma unroll 1
-  for (int t = 0; t < T; ++t) {
-    if (t + S - 2 < T) wait_loads<(S - 2) * LPT>();
-    else wait_loads<0>();
-    if (nch) clear_ragged(t, stage);
+  for (int j = 0; j < 4; ++j) hslot[j] = ((2 * j + lg) ^ ((ln % HRB >> 1) & 7)) * 16;
+  auto read_h = [&](int stage, int j, int i) __attribute__((always_inline)) {
+    const uint32_t slot = HRB == 8 && (i & 1) ? hslot[j] ^ 64u : hslot[j];
+    return *reinterpret_cast<const u32x4*>(hrows + stage * K::STAGE + i * HRB * 128 + slot);
+  };
+  auto fetch = [&](int parity, int stage, uint32_t keep, Operands& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) x.w[c] = *reinterpret_cast<const u32x4*>(lds + stage * K::STAGE + (wave * NC + c) * 1024 + lane * 16);
+#pragma unroll
+    for (int half = 0; half < PER; ++half) {
+      const uint2* const hs = hsum + ((parity * WK + part) * 2 + half) * K::HROWS + ln % HRB;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) x.rows[half][i] = hs[i * HRB];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        // (a half past the end of k has no group: its sums are zeros)
+        const unsigned char* const from = scales + (c * q.groups + min(g, q.groups - 1)) * (kTileCols * esize);
+        x.scale[half][c] = (ZEROS ? *reinterpret_cast<const uint32_t*>(from) : *reinterpret_cast<const uint16_t*>(from)) & keep;
+      }
+      left -= STEP / 2;
+      if (left == 0) {
+        ++g;
+        left = per_group;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) x.h[j][i] = read_h(stage, j, i);
+  };
+  f32x16 sum[NC][NB];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) sum[c][i] = f32x16{};
+  // Products of a group and column tile go to one set of accumulators while those of the one before are scaled and added up in
+  // the other, between the MFMAs: the wavefronts run in step, so what one does not overlap by itself is hardly overlapped at all.
+  constexpr int SETS = NC * PER > 1 ? 2 : 1;
+  auto compute = [&](const Operands& x, int stage, auto&& midway) __attribute__((always_inline)) {
+    u32x4 later[2][NB];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) later[j][i] = read_h(stage, j + 2, i);
+    f32x16 acc[SETS][NB];
+    float scale = 0.f;
+    static_for<NC * PER>([&](auto pp) __attribute__((always_inline)) {
+      constexpr int P = decltype(pp)::value, c = P / PER, half = P % PER, SET = P % SETS, BEFORE = (P + NC * PER - 1) % (NC * PER) / PER;
+      const uint32_t o = ZEROS ? (x.scale[half][c] >> 16 ^ 0x8000u) : 0xC1C0u;  // -(16 + o): -24 without zero points
+      u32x4 b{lg == 0 ? o | o << 16 : 0u, lg == 0 ? o : 0u, 0u, 0u};
+      if constexpr (P > 0 && P == NC * PER - 1) midway();
+      constexpr int M = (STEP + 1) * NB;
+      static_for<M>([&](auto mm) __attribute__((always_inline)) {
+        constexpr int m = decltype(mm)::value, j = half * STEP + m / NB - 1, i = m % NB;
+        if constexpr (m < NB) acc[SET][i] = mfma(u32x4{x.rows[half][i].x, x.rows[half][i].y, 0u, 0u}, b, f32x16{});
+        else acc[SET][i] = mfma(j < 2 ? x.h[j & 1][i] : later[j & 1][i], b, acc[SET][i]);
+        if constexpr (i == NB - 1 && m < M - 1) b = codes_to_bf16(x.w[c][j + 1]);
+        if constexpr (P > 0) {
+          constexpr int E0 = NB * 16 * m / M, E1 = NB * 16 * (m + 1) / M;
+          static_for<E1 - E0>([&](auto ee) __attribute__((always_inline)) {
+            constexpr int e = E0 + decltype(ee)::value;
+            sum[BEFORE][e / 16][e % 16] = __builtin_fmaf(scale, acc[SETS - 1 - SET][e / 16][e % 16], sum[BEFORE][e / 16][e % 16]);
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      });
+      scale = __uint_as_float(x.scale[half][c] << 16);
+    });
+    if constexpr (NC * PER == 1) midway();
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum[NC - 1][i][e] = __builtin_fmaf(scale, acc[SETS - 1][i][e], sum[NC - 1][i][e]);
+  };
+
+  // Step t.  Its barrier says that the wavefronts are done with step t - 1 and that step t + 1's rows and their sums are in LDS, whose
+  // first operands are fetched under this step's MFMAs.  The rows of step t + S - 1 go to the stage of step t - 1, and the weights
+  // of step t + S to this wavefront's part of stage t, which it has in registers: they come from further away.  Late in the step
+  // the rows of step t + 2, loaded by then, are added up.
+  constexpr int MAY_FLY = (S - 3) * HL + (S - 2) * NC;   // loads issued behind the rows of step t + 2
+  int h_ahead = rot, w_ahead = rot;                      // indices of the blocks to be loaded next
+#pragma unroll
+  for (int t = 0; t < S; ++t) {
+    if (t < S - 1 && t < T) {
+      load_h(h_ahead, t);
+      h_ahead = next_of(h_ahead);
+    }
+    if (t < T) {
+      load_w(w_ahead, t);
+      w_ahead = next_of(w_ahead);
+    }
+  }
+  // the rows of steps 0 and 1
+  if (S <= T) wait_loads<MAY_FLY + NC>();
+  else wait_loads<0>();
+  int now = rot, rows_at = rot;                          // indices of the blocks to be multiplied and to be added up next
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    if (t < T) {
+      if (nch) clear_ragged(rows_at, t);
+      add_rows(t, t);
+      rows_at = next_of(rows_at);
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  hard_fence();
+  // (what a part loads in the place of a block that it has not gets a scale of 0)
+  auto keep = [&](int at) { return at < count ? 0xFFFFFFFFu : 0xFFFF0000u; };
+  Operands x[2];
+  group_at(kb0 + rot);
+  fetch(0, 0, keep(now), x[0]);
+  int stage = 0;
+  auto step = [&](auto odd, int t) __attribute__((always_inline)) {
+    constexpr int ODD = decltype(odd)::value;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     hard_fence();
-    if (t + S - 1 < T) load(t + S - 1, next);
-    if (t < count) compute(kb0 + t, stage);
-    hard_fence();
-    stage = stage + 1 == S ? 0 : stage + 1;
-    next = next + 1 == S ? 0 : next + 1;
+    const int then = next_of(now), one = stage + 1 == S ? 0 : stage + 1, two = one + 1 == S ? 0 : one + 1, last = stage == 0 ? S - 1 : stage - 1;
+    if (t + S - 1 < T) {
+      load_h(h_ahead, last);
+      h_ahead = next_of(h_ahead);
+    }
+    if (t + S < T) {
+      load_w(w_ahead, stage);
+      w_ahead = next_of(w_ahead);
+    }
+    if (then == 0) group_at(kb0);
+    fetch(1 - ODD, one, keep(then), x[1 - ODD]);         // (behind the last step: something that nobody uses)
+    compute(x[ODD], stage, [&]() __attribute__((always_inline)) {
+      if (t + 2 >= T) return;
+      if (t + S < T) wait_loads<MAY_FLY>();
+      else wait_loads<0>();
+      if (nch) clear_ragged(rows_at, two);
+      add_rows(ODD, two);
+      rows_at = next_of(rows_at);
+    });
+    now = then;
+    stage = one;
+  };
+#pragma unroll 1
+  for (int t = 0; t < T; t += 2) {
+    step(IntT<0>{}, t);
+    if (t + 1 < T) step(IntT<1>{}, t + 1);
   }
   // ---- the parts of k added up, guidance mix, temperature, z ----------------------------------------------------
   if (tid < RB * 32) table[tid] = row_dest(a, mine);
   __syncthreads();
   float* const red = reinterpret_cast<float*>(lds);
-  const int v = tile * kTileCols + ln;
   if constexpr (WK > 1) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) red[((wave * NB + i) * 16 + e) * 64 + lane] = sum[i][e];
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) red[(((wave * NC + c) * NB + i) * 16 + e) * 64 + lane] = sum[c][i][e];
     __syncthreads();
   }
-  if (v >= a.n) return;
   static_assert(16 % WK == 0, "elements per part");
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
+  for (int c = 0; c < NC; ++c) {
+    const int v = (tile + c) * kTileCols + ln;
+    if (v >= a.n) continue;
 #pragma unroll
-    for (int ee = 0; ee < 16 / WK; ++ee) {
-      // the wavefronts of a tile store a share of its elements each
-      const int e = WK > 1 ? part + ee * WK : ee;
-      float c, u;
-      if constexpr (WK > 1) {
-        c = u = 0.f;
+    for (int r = 0; r < RB; ++r)
 #pragma unroll
-        for (int p = 0; p < WK; ++p) {
-          c += red[(((p * WC + wc) * NB + r * C) * 16 + e) * 64 + lane];
-          u += red[(((p * WC + wc) * NB + r * C + C - 1) * 16 + e) * 64 + lane];
+      for (int ee = 0; ee < 16 / WK; ++ee) {
+        // the wavefronts of a tile store a share of its elements each
+        const int e = WK > 1 ? part + ee * WK : ee;
+        float cond, uncond;
+        if constexpr (WK > 1) {
+          cond = uncond = 0.f;
+#pragma unroll
+          for (int p = 0; p < WK; ++p) {
+            const float* const from = red + (((p * WC + wc) * NC + c) * NB + r * C) * 1024 + e * 64 + lane;
+            cond += from[0];
+            uncond += from[(C - 1) * 1024];
+          }
+        } else {
+          cond = sum[c][r * C][ee];
+          uncond = sum[c][r * C + C - 1][ee];
         }
-      } else {
-        c = sum[r * C][ee];
-        u = sum[r * C + C - 1][ee];
+        const int row = table[r * 32 + (e >> 2) * 8 + lg * 4 + (e & 3)];
+        if (row >= 0) a.z[static_cast<int64_t>(row) * a.n + v] = processed_logit<C>(a, cond, uncond);
       }
-      const int row = table[r * 32 + (e >> 2) * 8 + lg * 4 + (e & 3)];
-      if (row >= 0) a.z[static_cast<int64_t>(row) * a.n + v] = processed_logit<C>(a, c, u);
-    }
+  }
 }
 
 // ---- quantisation and layout ---------------------------------------------------------------------------
@@ -309,30 +456,41 @@ inline int k_blocks(int d) { return (d + kBlockK - 1) / kBlockK; }
 
 template <class K>
 bool scales_fit(const QuantizedArgs& q) {
-  return up(static_cast<int64_t>(K::WC) * q.groups * kTileCols * (q.zeros ? 4 : 2), 1024) <= K::SCALES;
+  return up(static_cast<int64_t>(K::COLTILES) * q.groups * kTileCols * (q.zeros ? 4 : 2), 1024) <= K::SCALES;
+}
+template <class K, int STEP>
+void launch_step(const LmHeadArgs& a, const QuantizedArgs& q, dim3 grid, int WT, int MT, hipStream_t s) {
+  if (q.zeros) hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, true>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
+  else hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, false>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
 }
 template <class K>
 hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
   const int64_t tiles = up(a.n, kTileCols) / kTileCols;
-  const int WT = static_cast<int>((tiles + K::WC - 1) / K::WC), MT = (a.B * a.L + K::RB * 32 - 1) / (K::RB * 32);
-  const dim3 grid((WT + 7) / 8 * 8 * MT), block(K::THREADS);
-  if (q.group % kBlockK == 0) hipLaunchKernelGGL((lm_head_quantized_kernel<K, 4>), grid, block, 0, s, a, q, WT, MT);
-  else hipLaunchKernelGGL((lm_head_quantized_kernel<K, 2>), grid, block, 0, s, a, q, WT, MT);
+  const int WT = static_cast<int>((tiles + K::COLTILES - 1) / K::COLTILES), MT = (a.B * a.L + K::RB * 32 - 1) / (K::RB * 32);
+  const dim3 grid((WT + 7) / 8 * 8 * MT);
+  if (q.group % kBlockK == 0) launch_step<K, 4>(a, q, grid, WT, MT, s);
+  else launch_step<K, 2>(a, q, grid, WT, MT, s);
   return hipGetLastError();
 }
+static_assert(QuantCfg<2, 1, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4 && QuantCfg<1, 2, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4,
+              "the scales of one column tile always fit");
 // In how many parts k is dealt over the wavefronts of a workgroup: as few as leave enough workgroups, and as let the scales
 // of its columns fit.
-static_assert(QuantCfg<2, 1, 32, 4, 4>::SCALES >= kMaxGroups * kTileCols * 4 && QuantCfg<1, 2, 32, 4, 4>::SCALES >= kMaxGroups * kTileCols * 4,
-              "the scales of one column tile always fit");
 template <int C, int RB, int HRB>
 hipError_t launch_parts(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
   const int64_t tiles = up(a.n, kTileCols) / kTileCols, row_tiles = (a.B * a.L + RB * 32 - 1) / (RB * 32);
   const int64_t work = tiles * row_tiles;
-  using One = QuantCfg<C, RB, HRB, 8, 1>;
-  using Two = QuantCfg<C, RB, HRB, 8, 2>;
-  using Four = QuantCfg<C, RB, HRB, 4, 4>;
-  if (work >= 2048 && scales_fit<One>(q)) return launch<One>(a, q, s);
-  if (work >= 1024 && scales_fit<Two>(q)) return launch<Two>(a, q, s);
+  using Wide = QuantCfg<C, RB, HRB, 2, 8, 2, 160>;
+  using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
+  using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
+  using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
+  if (work >= 1536 && scales_fit<Wide>(q)) return launch<Wide>(a, q, s);
+  if (work >= 1536 && scales_fit<One>(q)) return launch<One>(a, q, s);
+  if (work >= 768 && scales_fit<Two>(q)) return launch<Two>(a, q, s);
+  if constexpr (HRB == 8) {
+    using Small = QuantCfg<C, RB, HRB, 1, 4, 4, 80>;
+    if (scales_fit<Small>(q)) return launch<Small>(a, q, s);
+  }
   return launch<Four>(a, q, s);
 }
 
