@@ -351,8 +351,9 @@ __global__ __launch_bounds__(256) void finish_kernel(const float2* __restrict__ 
 
 // ---- the largest elements ----------------------------------------------------------------------------
 // Per workgroup the largest magnitude (as an integer: the order is the same) among the finite elements of its share of W,
-// of the rows of h and of their weights; settle_kernel takes the largest of those.
-constexpr int kRangeBlocks = 1024;
+// of the rows of h and of their weights.  The workgroups that turn the rows of h take the largest of those, each for itself, and
+// the first leaves the exponents for the kernels behind it; settle_kernel where no rows are turned.
+constexpr int kRangeBlocks = 512;
 __device__ __forceinline__ uint32_t finite_magnitude16(uint32_t two) {            // the larger of two bf16 values'
   const uint32_t a = two & 0x7FFFu, b = two >> 16 & 0x7FFFu;
   return max(a < 0x7F80u ? a : 0u, b < 0x7F80u ? b : 0u);
@@ -396,8 +397,8 @@ __global__ __launch_bounds__(256) void range_kernel(const u32x4* __restrict__ W,
   g = block_max<4>(g, words);
   if (threadIdx.x == 0) out[blockIdx.x] = make_uint3(w, x, g);
 }
-__global__ __launch_bounds__(256) void settle_kernel(const uint3* __restrict__ in, int blocks, Exponents* __restrict__ out) {
-  __shared__ uint32_t words[4];
+// the largest of them all, by a workgroup of 256
+__device__ __forceinline__ Exponents settle(const uint3* in, int blocks, uint32_t* words) {
   uint32_t w = 0u, x = 0u, g = 0u;
   for (int i = threadIdx.x; i < blocks; i += 256) {
     const uint3 v = in[i];
@@ -408,21 +409,37 @@ __global__ __launch_bounds__(256) void settle_kernel(const uint3* __restrict__ i
   w = block_max<4>(w, words);
   x = block_max<4>(x, words);
   g = block_max<4>(g, words);
-  if (threadIdx.x == 0)
-    *out = Exponents{static_cast<int>(w >> 7) - 127, static_cast<int>(x >> 7) - 127, static_cast<int>(g >> 23) - 127};
+  return Exponents{static_cast<int>(w >> 7) - 127, static_cast<int>(x >> 7) - 127, static_cast<int>(g >> 23) - 127};
+}
+__global__ __launch_bounds__(256) void settle_kernel(const uint3* __restrict__ in, int blocks, Exponents* __restrict__ out) {
+  __shared__ uint32_t words[4];
+  const Exponents e = settle(in, blocks, words);
+  if (threadIdx.x == 0) *out = e;
 }
 
 // ---- to[c][r] = from[r][c] * 2^(kTop - exponent) in fp16 for r < rows, 0 for r up to rows_pad and where marks[r] < 0 ------
+// ROWS: the rows of h, the exponents from `ranges`; else W, the exponents from `exps`.
 constexpr int kTurn = 64;
+template <bool ROWS>
 __global__ __launch_bounds__(256) void turn_kernel(const uint16_t* __restrict__ from, int64_t ld_from, int rows, int cols,
                                                    uint16_t* __restrict__ to, int64_t ld_to, int rows_pad,
-                                                   const int32_t* __restrict__ marks, const int* __restrict__ exponent) {
+                                                   const int32_t* __restrict__ marks, const uint3* __restrict__ ranges, int blocks,
+                                                   Exponents* __restrict__ exps) {
   __shared__ uint16_t tile[kTurn][kTurn + 2];
-  const int r0 = blockIdx.x * kTurn, c0 = blockIdx.y * kTurn, up = kTop - *exponent;
+  __shared__ uint32_t words[4];
+  const int r0 = blockIdx.x * kTurn, c0 = blockIdx.y * kTurn;
+  int up;
+  if constexpr (ROWS) {
+    const Exponents e = settle(ranges, blocks, words);
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *exps = e;
+    up = kTop - e.h;
+  } else {
+    up = kTop - exps->W;
+  }
   for (int p = threadIdx.x; p < kTurn * kTurn / 8; p += 256) {
     const int r = p / (kTurn / 8), c = p % (kTurn / 8) * 8;
     u32x4 v{0u, 0u, 0u, 0u};
-    if (r0 + r < rows && c0 + c < cols && !(marks && marks[r0 + r] < 0))
+    if (r0 + r < rows && c0 + c < cols && !(ROWS && marks[r0 + r] < 0))
       v = *reinterpret_cast<const u32x4*>(from + static_cast<int64_t>(r0 + r) * ld_from + c0 + c);
     uint32_t* const at = reinterpret_cast<uint32_t*>(&tile[r][c]);
 #pragma unroll
@@ -497,11 +514,12 @@ hipError_t launch_gemm(GemmArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool ROWS>
 hipError_t launch_turn(const uint16_t* from, int64_t ld_from, int rows, int cols, uint16_t* to, int64_t ld_to, int rows_pad,
-                       const int32_t* marks, const int* exponent, hipStream_t s) {
+                       const int32_t* marks, const uint3* ranges, int blocks, Exponents* exps, hipStream_t s) {
   if (rows_pad == 0) return hipSuccess;
-  hipLaunchKernelGGL(turn_kernel, dim3((rows_pad + kTurn - 1) / kTurn, (cols + kTurn - 1) / kTurn), dim3(256), 0, s, from, ld_from, rows, cols, to,
-                     ld_to, rows_pad, marks, exponent);
+  hipLaunchKernelGGL(turn_kernel<ROWS>, dim3((rows_pad + kTurn - 1) / kTurn, (cols + kTurn - 1) / kTurn), dim3(256), 0, s, from, ld_from, rows,
+                     cols, to, ld_to, rows_pad, marks, ranges, blocks, exps);
   return hipGetLastError();
 }
 
@@ -519,7 +537,6 @@ Plan make_plan(int rows, int n, int d, bool f32) {
   const int64_t per_column = 2 * (rows + p.mpad * (f32 ? 2 : 1) + d);
   int64_t piece = kPieceBytes / per_column / 256 * 256;
   if (piece < 256) piece = 256;
-  if (piece > 16384) piece = 16384;
   // pieces of one size
   const int64_t count = (n + piece - 1) / piece;
   piece = up((n + count - 1) / count, 256);
@@ -584,10 +601,14 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
   const int blocks = static_cast<int>(want < 1 ? 1 : want < kRangeBlocks ? want : kRangeBlocks);
   hipLaunchKernelGGL(range_kernel, dim3(blocks), dim3(256), 0, s, reinterpret_cast<const u32x4*>(c.W), pieces,
                      reinterpret_cast<const u32x4*>(c.h), c.rows, c.d / 8, c.weight, c.targets, ranges);
-  hipLaunchKernelGGL(settle_kernel, dim3(1), dim3(256), 0, s, ranges, blocks, exps);
-  hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
+  if (c.dW && c.rows > 0) {
+    e = launch_turn<true>(c.h, c.d, c.rows, c.d, hT, p.mpad, static_cast<int>(p.mpad), c.targets, ranges, blocks, exps, s);
+  } else {
+    hipLaunchKernelGGL(settle_kernel, dim3(1), dim3(256), 0, s, ranges, blocks, exps);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
-  if (c.dW && (e = launch_turn(c.h, c.d, c.rows, c.d, hT, p.mpad, static_cast<int>(p.mpad), c.targets, &exps->h, s)) != hipSuccess) return e;
   const int terms = c.f32 ? 2 : 1;
   for (int v0 = 0; v0 < c.n; v0 += p.piece) {
     const int v = c.n - v0 < p.piece ? c.n - v0 : p.piece;
@@ -605,7 +626,7 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
       if ((e = launch_gemm<kGradient>(a, s)) != hipSuccess) return e;
     }
     if (c.dh && c.rows > 0) {
-      if ((e = launch_turn(W, c.d, v, c.d, WT, vpad, static_cast<int>(vpad), nullptr, &exps->W, s)) != hipSuccess) return e;
+      if ((e = launch_turn<false>(W, c.d, v, c.d, WT, vpad, static_cast<int>(vpad), nullptr, nullptr, 0, exps, s)) != hipSuccess) return e;
       GemmArgs a{};
       a.A = dz; a.B = WT; a.lda = a.ldb = vpad;
       a.M = c.rows; a.N = c.d; a.KT = static_cast<int>(vpad / 64); a.wrapB = 0x7FFFFFFF; a.KS = p.parts;

@@ -5,9 +5,9 @@
 //
 // Gradient.  The rows that share an id have to be added up in 32 bits, in a fixed order, and every row of dW is written
 // once.  So the row numbers are sorted by id (a stable radix sort: equal ids keep the order of their rows), and a
-// wavefront walks kChunk of the sorted rows along 512 columns.  An id whose rows lie in one chunk is done there; one
-// that reaches over a chunk's border leaves a partial sum per chunk, and join_kernel adds those up, in order, by eight
-// wavefronts each: one id may hold most of the rows.  Ids that no row has get their zeros in the same launch as the sums,
+// wavefront walks a chunk of the sorted rows along 512 columns.  An id whose rows lie in one chunk is done there; one
+// that reaches over a chunk's border leaves a partial sum per chunk, and join_kernel adds those up, in order, by several
+// wavefronts: one id may hold most of the rows.  Ids that no row has get their zeros in the same launch as the sums,
 // from workgroups that look their stretch of ids up in the sorted list.
 #include "scd_device.h"
 #include "scd_kernels.h"
@@ -85,17 +85,20 @@ __device__ __forceinline__ uint64_t equal_digits(uint32_t digit, int bits, uint6
   }
   return m;
 }
-// One pass over the block's keys in k[], r[] (ROUNDS per thread; `count` of the block exist): their digits' bins are
-// counted per wavefront in `bins` [NW][kMaxBins], and place[] = number of equal digits before the key in its wavefront.
+// One pass over the block's keys in k[] (`rounds` of the ROUNDS per thread in use, `count` of the block exist; a wavefront holds
+// rounds * 64 neighbours): their digits' bins are counted per wavefront in `bins` [NW][kMaxBins], and place[] = number of
+// equal digits before the key in its wavefront.
 template <int NW, int ROUNDS>
-__device__ __forceinline__ void count_digits(const uint32_t (&k)[ROUNDS], const Digits g, int count, uint32_t* bins, uint32_t (&place)[ROUNDS]) {
+__device__ __forceinline__ void count_digits(const uint32_t (&k)[ROUNDS], const Digits g, int rounds, int count, uint32_t* bins,
+                                             uint32_t (&place)[ROUNDS]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i < NW * kMaxBins; i += NW * 64) bins[i] = 0u;
+  for (int b = lane; b < 1 << g.bits; b += 64) bins[wave * kMaxBins + b] = 0u;
   __syncthreads();
   uint32_t* const mine = bins + wave * kMaxBins;
 #pragma unroll
   for (int j = 0; j < ROUNDS; ++j) {
-    const bool is = wave * ROUNDS * 64 + j * 64 + lane < count;
+    if (j >= rounds) break;
+    const bool is = wave * rounds * 64 + j * 64 + lane < count;
     const uint64_t live = __builtin_amdgcn_ballot_w64(is);
     const uint32_t digit = (k[j] >> g.shift) & ((1u << g.bits) - 1u);
     const uint64_t same = equal_digits(digit, g.bits, live);
@@ -110,14 +113,15 @@ __device__ __forceinline__ void count_digits(const uint32_t (&k)[ROUNDS], const 
 // bins [NW][kMaxBins] -> first place of a wavefront's digit in the sorted block, given the first place of every digit in
 // `first` (kMaxBins words; the block's totals are added by the caller's scan before)
 template <int NW>
-__device__ __forceinline__ void spread_bins(uint32_t* bins, const uint32_t* first) {
-  for (int b = threadIdx.x; b < kMaxBins; b += NW * 64) {
-    uint32_t at = first[b];
+__device__ __forceinline__ void spread_bins(uint32_t* bins, const uint32_t* first, int nbins) {
+  for (int b = threadIdx.x; b < nbins; b += NW * 64) {
+    uint32_t at = first[b], c[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) c[w] = bins[w * kMaxBins + b];
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const uint32_t c = bins[w * kMaxBins + b];
       bins[w * kMaxBins + b] = at;
-      at += c;
+      at += c[w];
     }
   }
   __syncthreads();
@@ -157,7 +161,8 @@ __global__ __launch_bounds__(kOneWaves * 64) void sort_one_kernel(const int32_t*
   __shared__ uint32_t bins[kOneWaves * kMaxBins], first[kMaxBins];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t k[kOneRounds], r[kOneRounds], place[kOneRounds];
-  auto at = [&](int j) { return wave * kOneRounds * 64 + j * 64 + lane; };
+  const int rounds = (rows + kOneWaves * 64 - 1) / (kOneWaves * 64);
+  auto at = [&](int j) { return j < rounds ? wave * rounds * 64 + j * 64 + lane : rows; };
 #pragma unroll
   for (int j = 0; j < kOneRounds; ++j) {
     r[j] = at(j);
@@ -165,15 +170,16 @@ __global__ __launch_bounds__(kOneWaves * 64) void sort_one_kernel(const int32_t*
   }
   for (int p = 0; p < passes; ++p) {
     const Digits g{p * bits, bits};
-    count_digits<kOneWaves, kOneRounds>(k, g, rows, bins, place);
+    count_digits<kOneWaves, kOneRounds>(k, g, rounds, rows, bins, place);
     for (int b = tid; b < kMaxBins; b += kOneWaves * 64) {
       uint32_t sum = 0u;
+      if (b < 1 << bits)
 #pragma unroll
       for (int w = 0; w < kOneWaves; ++w) sum += bins[w * kMaxBins + b];
       first[b] = sum;
     }
     scan_bins(first);
-    spread_bins<kOneWaves>(bins, first);
+    spread_bins<kOneWaves>(bins, first, 1 << bits);
 #pragma unroll
     for (int j = 0; j < kOneRounds; ++j)
       if (at(j) < rows) block[bins[wave * kMaxBins + ((k[j] >> g.shift) & ((1u << bits) - 1u))] + place[j]] = KeyRow{k[j], r[j]};
@@ -244,18 +250,21 @@ __global__ __launch_bounds__(kWaves * 64) void sort_move_kernel(const int32_t* _
     const int b = threadIdx.x + i * kWaves * 64;
     uint32_t all = 0u;
     before[i] = 0u;
-    for (int blk = 0; blk < static_cast<int>(gridDim.x); ++blk) {
-      const uint32_t c = counts[static_cast<int64_t>(blk) * kMaxBins + b];
-      before[i] += blk < static_cast<int>(blockIdx.x) ? c : 0u;
-      all += c;
+    if (b < 1 << g.bits) {
+#pragma unroll 16
+      for (int blk = 0; blk < static_cast<int>(gridDim.x); ++blk) {
+        const uint32_t c = counts[static_cast<int64_t>(blk) * kMaxBins + b];
+        before[i] += blk < static_cast<int>(blockIdx.x) ? c : 0u;
+        all += c;
+      }
     }
     first[b] = all;
   }
   scan_bins(first);
 #pragma unroll
   for (int i = 0; i < kMaxBins / (kWaves * 64); ++i) first[threadIdx.x + i * kWaves * 64] += before[i];
-  count_digits<kWaves, kRounds>(k, g, count, bins, place);
-  spread_bins<kWaves>(bins, first);
+  count_digits<kWaves, kRounds>(k, g, kRounds, count, bins, place);
+  spread_bins<kWaves>(bins, first, 1 << g.bits);
 #pragma unroll
   for (int j = 0; j < kRounds; ++j)
     if (wave * kRounds * 64 + j * 64 + lane < count)
@@ -291,6 +300,7 @@ struct SumArgs {
   void* dW;
   float* part;          // [chunks][2][d]: sums of the chunk's first id (it began before the chunk) and of its last (it goes on)
   int rows, V, d, chunk, chunks, zero_blocks, zero_ids;
+  uint32_t sum_blocks;
   float scale;
 };
 
@@ -301,10 +311,10 @@ __device__ __forceinline__ uint32_t key_at(const SumArgs& a, int64_t at) { retur
 template <bool F32, bool ACC>
 __global__ __launch_bounds__(256) void sum_kernel(const SumArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (!ACC && static_cast<int>(blockIdx.x) < a.zero_blocks) {
+  if (!ACC && blockIdx.x >= a.sum_blocks) {
     // ---- rows that no id has: a workgroup looks after zero_ids neighbouring ids of dW --------------------
     __shared__ uint32_t seen[kMaxBins];
-    const uint32_t v0 = blockIdx.x * a.zero_ids, v1 = min(v0 + a.zero_ids, static_cast<uint32_t>(a.V));
+    const uint32_t v0 = (blockIdx.x - a.sum_blocks) * a.zero_ids, v1 = min(v0 + a.zero_ids, static_cast<uint32_t>(a.V));
     for (int i = threadIdx.x; i < a.zero_ids; i += 256) seen[i] = 0u;
     __syncthreads();
     // the first sorted row with a key of v0 or more, 64 places at a time
@@ -334,7 +344,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const SumArgs a) {
   }
   // ---- a chunk of the sorted rows along 512 columns ------------------------------------------------------
   const int slices = (a.d + kSlice - 1) / kSlice;
-  const int64_t item = static_cast<int64_t>(blockIdx.x - (ACC ? 0 : a.zero_blocks)) * 4 + wave;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + wave;
   if (item >= static_cast<int64_t>(a.chunks) * slices) return;
   const int chunk = static_cast<int>(item / slices), col = static_cast<int>(item % slices) * kSlice + lane * 8;
   const bool mine = col < a.d;
@@ -377,56 +387,70 @@ __global__ __launch_bounds__(256) void sum_kernel(const SumArgs a) {
   flush(behind != key);
 }
 
-// The ids that reach over chunks' borders: the workgroup of the chunk in which such an id begins adds its partial sums up.
+// The ids that reach over chunks' borders: a workgroup for the chunk in which such an id begins and 512 columns adds its partial
+// sums up.  They come from other XCDs, 2 to 4 us a round trip, so its wavefronts share them (a fifth of 25600 rows along 4096
+// columns in one id: one wavefront in two 56 us, one in eight 14).
+constexpr int kJoinWaves = 8;
 template <bool F32, bool ACC>
-__global__ __launch_bounds__(512) void join_kernel(const SumArgs a) {
-  constexpr int NW = 8;
-  __shared__ f32x8 sums[NW][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int chunk = blockIdx.x, col = blockIdx.y * kSlice + lane * 8;
+__global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(const SumArgs a) {
+  constexpr int split = kJoinWaves;
+  __shared__ f32x8 sums[kJoinWaves][64];
+  __shared__ int run[kJoinWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = blockIdx.x;
   const int64_t p0 = static_cast<int64_t>(chunk) * a.chunk, p1 = p0 + a.chunk;
   if (p1 >= a.rows) return;
-  const uint32_t key = a.sorted[p1 - 1].key;
-  if (key >= static_cast<uint32_t>(a.V) || a.sorted[p1].key != key) return;       // it ends here
-  if (a.sorted[p0].key == key && key_at(a, p0 - 1) == key) return;                // it began before
-  // chunks behind this one that begin with the id: all up to the last one, found 64 at a time
+  const uint32_t key = a.sorted[p1 - 1].key, behind = a.sorted[p1].key, first_key = a.sorted[p0].key, before = key_at(a, p0 - 1);
+  if (key >= static_cast<uint32_t>(a.V) || behind != key) return;       // it ends here
+  if (first_key == key && before == key) return;                         // it began before
+  // chunks behind this one that begin with the id: all up to the last one, found kJoinWaves * 64 at a time
   int last = chunk + 1;
   for (;;) {
-    const int c = last + 1 + lane;
-    const uint64_t same = __builtin_amdgcn_ballot_w64(c < a.chunks && a.sorted[static_cast<int64_t>(c) * a.chunk].key == key);
-    const int n = same == ~0ull ? 64 : __builtin_ctzll(~same);
+    const int c = last + 1 + wave * 64 + lane;
+    const uint64_t same = __builtin_amdgcn_ballot_w64(c < a.chunks && a.sorted[min(static_cast<int64_t>(c) * a.chunk, static_cast<int64_t>(a.rows) - 1)].key == key);
+    if (lane == 0) run[wave] = same == ~0ull ? 64 : __builtin_ctzll(~same);
+    __syncthreads();
+    int n = 0;
+    for (int w = 0; w < kJoinWaves; ++w) {
+      n += run[w];
+      if (run[w] < 64) break;
+    }
+    __syncthreads();
     last += n;
-    if (n < 64) break;
+    if (n < kJoinWaves * 64) break;
   }
+  const int first = chunk + 1, count = last - first + 1, per = (count + split - 1) / split, share = wave;
+  const int c0 = first + share * per, c1 = min(c0 + per, last + 1);
+  const int col = blockIdx.y * kSlice + lane * 8;
   const bool mine = col < a.d;
-  const int first = chunk + 1, count = last - first + 1, per = (count + NW - 1) / NW;
-  const int c0 = first + wave * per, c1 = min(c0 + per, last + 1);
   f32x8 sum{};
   if (mine) {
     const float* const at = a.part + col;
-    if (wave == 0) sum = *reinterpret_cast<const f32x8*>(at + (static_cast<int64_t>(chunk) * 2 + 1) * a.d);
+    if (share == 0) sum = *reinterpret_cast<const f32x8*>(at + (static_cast<int64_t>(chunk) * 2 + 1) * a.d);
 #pragma unroll 8
     for (int c = c0; c < c1; ++c) sum += *reinterpret_cast<const f32x8*>(at + static_cast<int64_t>(c) * 2 * a.d);
   }
   sums[wave][lane] = sum;
   __syncthreads();
-  if (wave != 0 || !mine) return;
+  if (share != 0 || !mine) return;
 #pragma unroll
-  for (int w = 1; w < NW; ++w) sum += sums[w][lane];
+  for (int w = 1; w < split; ++w) sum += sums[wave + w][lane];
   put<F32, ACC>(a.dW, key, a.d, col, sum * a.scale);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 // sorted rows of a wavefront
-inline int chunk_rows(int rows) { return rows > (1 << 16) ? 128 : 32; }
+inline int chunk_rows(int rows) { return rows > (1 << 16) ? 128 : rows > (1 << 14) ? 64 : 32; }
 
 template <bool F32, bool ACC>
-hipError_t launch_sums(const SumArgs& a, hipStream_t s) {
+hipError_t launch_sums(SumArgs a, hipStream_t s) {
   const int slices = (a.d + kSlice - 1) / kSlice;
-  const int64_t blocks = (static_cast<int64_t>(a.chunks) * slices + 3) / 4 + (ACC ? 0 : a.zero_blocks);
+  // the sums first: they wait for loads, and the zeros fill the time
+  a.sum_blocks = static_cast<uint32_t>((static_cast<int64_t>(a.chunks) * slices + 3) / 4);
+  const int64_t blocks = static_cast<int64_t>(a.sum_blocks) + (ACC ? 0 : a.zero_blocks);
   if (blocks == 0) return hipSuccess;
   hipLaunchKernelGGL((sum_kernel<F32, ACC>), dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, s, a);
-  if (a.chunks > 1) hipLaunchKernelGGL((join_kernel<F32, ACC>), dim3(a.chunks - 1, slices), dim3(512), 0, s, a);
+  if (a.chunks > 1) hipLaunchKernelGGL((join_kernel<F32, ACC>), dim3(a.chunks - 1, slices), dim3(kJoinWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
@@ -488,7 +512,7 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& e, hipStream_t s) {
     }
   }
   a.sorted = sorted;
-  a.zero_ids = 64;
+  a.zero_ids = 16;
   a.zero_blocks = (e.V + a.zero_ids - 1) / a.zero_ids;
   if (e.f32) return e.accumulate ? launch_sums<true, true>(a, s) : launch_sums<true, false>(a, s);
   return e.accumulate ? launch_sums<false, true>(a, s) : launch_sums<false, false>(a, s);
