@@ -487,7 +487,7 @@ struct Shape {
 // Tiles of which one round of a workgroup per CU costs `cost`: as in the LM head's choice.
 Shape choose(int64_t M, int64_t N) {
   struct Option { int hr, bn, cost; };
-  constexpr Option options[] = {{128, 128, 27}, {256, 128, 40}, {256, 256, 73}};
+  constexpr Option options[] = {{128, 64, 18}, {128, 128, 27}, {256, 128, 40}, {256, 192, 56}, {256, 256, 73}};
   Shape best{128, 128};
   int64_t least = -1;
   for (const Option& o : options) {
@@ -508,7 +508,9 @@ hipError_t launch_gemm(GemmArgs a, hipStream_t s) {
   const int64_t all = static_cast<int64_t>(a.MT) * a.NT * a.KS;
   if (all == 0) return hipSuccess;
   const dim3 grid(static_cast<uint32_t>((all + 7) / 8 * 8)), block(512);
-  if (t.hr == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, USE>), grid, block, 0, s, a);
+  if (t.bn == 64) hipLaunchKernelGGL((gemm_kernel<128, 64, USE>), grid, block, 0, s, a);
+  else if (t.hr == 128) hipLaunchKernelGGL((gemm_kernel<128, 128, USE>), grid, block, 0, s, a);
+  else if (t.bn == 192) hipLaunchKernelGGL((gemm_kernel<256, 192, USE>), grid, block, 0, s, a);
   else if (t.bn == 128) hipLaunchKernelGGL((gemm_kernel<256, 128, USE>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((gemm_kernel<256, 256, USE>), grid, block, 0, s, a);
   return hipGetLastError();
@@ -558,7 +560,7 @@ Plan make_plan(int rows, int n, int d, bool f32) {
 }  // namespace
 
 size_t cross_entropy_bytes(int rows, int n, int) {
-  const size_t tiles = (static_cast<size_t>(n) + 127) / 128;         // the narrowest tile's
+  const size_t tiles = (static_cast<size_t>(n) + 63) / 64;           // the narrowest tile's
   return up256(sizeof(float2) * tiles * rows) + up256(sizeof(float) * rows) + 256;
 }
 

@@ -11,16 +11,16 @@ template <int HR_, int BN_>
 struct GemmTile {
   static constexpr int HR = HR_, BN = BN_;
   static constexpr int NW = 8, THREADS = NW * 64;
-  static constexpr int CW = HR * BN <= 128 * 128 ? 32 : 64;   // rows of B per wavefront
+  static constexpr int CW = HR * BN <= 128 * 128 ? 32 : BN == 192 ? 96 : 64;   // rows of B per wavefront
   static constexpr int NC = CW / 32;
   static constexpr int WCOL = BN / CW, WROW = NW / WCOL;
   static constexpr int RW = HR / WROW;                        // rows of A per wavefront
   static constexpr int NB = RW / 32;
   static constexpr int AL = HR / 8 / NW, BL = BN / 8 / NW;    // loads per wavefront and k-tile
   static constexpr int AB = HR * 128, BB = BN * 128;          // bytes per stage
-  static constexpr int SB = 3, SA = HR == 256 && BN == 256 ? 2 : 3;
+  static constexpr int SB = 3, SA = HR == 256 && BN > 128 ? 2 : 3;
   static constexpr int STAGES = SB * BB + SA * AB;
-  static_assert(WCOL * WROW == NW && STAGES <= 160 * 1024, "tile shape");
+  static_assert(WCOL * WROW == NW && WROW * RW == HR && WCOL * CW == BN && AL * NW * 8 == HR && BL * NW * 8 == BN && STAGES <= 160 * 1024, "tile shape");
 };
 
 // One operand as a workgroup reads it: its first row, `rows` of them exist (past them the last one is read, and what
