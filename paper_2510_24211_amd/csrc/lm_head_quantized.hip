@@ -15,8 +15,9 @@
 // the low half, odd k in the high half of the word).  The blocks of a tile follow each other; behind all of them, per tile
 // and group, the 32 columns' scales (2 bytes each; with zero points 4, the second two holding 16 + o as bf16).
 //
-// A workgroup of NW wavefronts owns NC * NW / WK neighbouring column tiles, NC per wavefront; WK wavefronts share tiles and take
-// 1/WK of k each (their sums are added up at the end in a fixed order).  Weights and h rows go from memory straight into
+// A workgroup of NW wavefronts owns NC * NW / (WK * WR) neighbouring column tiles, NC per wavefront; WK wavefronts share tiles and
+// rows and take 1/WK of k each (their sums are added up at the end in a fixed order), WR share tiles and take a part of the rows
+// each.  Weights and h rows go from memory straight into
 // LDS, S stages deep; a wavefront reads its own weights back, the h rows are shared.  The scales of the workgroup's columns are
 // fetched whole at the start.
 #include "lm_head_rows.h"
@@ -27,22 +28,23 @@ namespace {
 
 constexpr int kTileCols = 32, kBlockK = 64, kBlockBytes = 1024, kTilesPad = 8;
 
-// rows per block of 32 that are really loaded: HRB; blocks per workgroup (guidance included): NB; KB of LDS it may take: KB
-template <int C_, int RB_, int HRB_, int NC_, int NW_, int WK_, int KB_>
+// rows per block of 32 that are really loaded: HRB; blocks of rows (guidance included) per wavefront: NB; KB of LDS it may take: KB
+template <int C_, int RB_, int HRB_, int NC_, int NW_, int WK_, int KB_, int WR_ = 1>
 struct QuantCfg {
-  static constexpr int C = C_, RB = RB_, HRB = HRB_, NC = NC_, NW = NW_, WK = WK_, LDS = KB_ * 1024;
-  static constexpr int THREADS = NW * 64, WC = NW / WK, COLTILES = WC * NC, NB = RB * C;
-  static constexpr int HROWS = NB * HRB;                 // h rows per part of k
+  static constexpr int C = C_, RB = RB_, HRB = HRB_, NC = NC_, NW = NW_, WK = WK_, WR = WR_, LDS = KB_ * 1024;
+  static constexpr int THREADS = NW * 64, WC = NW / WK / WR, COLTILES = WC * NC, NB = RB * C / WR;
+  static constexpr int HROWS = RB * C * HRB;                 // h rows per part of k
   static constexpr int HI = WK * HROWS / 8;              // load instructions for the h rows of a step, all parts
   static constexpr int HL = (HI + NW - 1) / NW;          // per wavefront
-  static constexpr int WB = NW * NC * kBlockBytes, HB = WK * HROWS * 128, STAGE = WB + HB;
+  static constexpr int WP = COLTILES * WK, WL = (WP + NW - 1) / NW;      // blocks of weights of a step, per wavefront to be loaded
+  static constexpr int WB = WP * kBlockBytes, HB = WK * HROWS * 128, STAGE = WB + HB;
   static constexpr int FIT = (LDS - LDS / 6) / STAGE, S = FIT > 7 ? 7 : FIT;
   static constexpr int RED = WK > 1 ? NW * NC * NB * 16 * 64 * 4 : 0;      // sums of the parts of k, in the place of the stages
   static constexpr int BASE = S * STAGE > RED ? S * STAGE : RED;
   static constexpr int TABLE = RB * 32 * 4;
   static constexpr int SUMS = 2 * WK * 2 * HROWS * 8;    // rows' sums of two steps, of the halves of a block
   static constexpr int SCALES = LDS - TABLE - SUMS - BASE;          // room for the columns' scales
-  static_assert(S >= 3 && SCALES >= COLTILES * 1024, "LDS");
+  static_assert(NW % 2 == 0 && S >= 3 && SCALES >= COLTILES * 1024 && RB % WR == 0 && (WK == 1 || WR == 1), "LDS");
 };
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
@@ -57,7 +59,7 @@ __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t w) {
 // STEP: MFMAs between two applications of a scale (2: groups that end inside a block of k, 4: they do not)
 template <class K, int STEP, bool ZEROS>
 __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmHeadArgs a, const QuantizedArgs q, const int WT, const int MT) {
-  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, WK = K::WK, WC = K::WC, NW = K::NW, S = K::S, HL = K::HL, HRB = K::HRB;
+  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, WL = K::WL, WR = K::WR, WK = K::WK, WC = K::WC, NW = K::NW, S = K::S, HL = K::HL, HRB = K::HRB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[K::LDS];
   int* const table = reinterpret_cast<int*>(lds + K::BASE);
   uint2* const hsum = reinterpret_cast<uint2*>(lds + K::BASE + K::TABLE);     // [2][WK][2][HROWS]
@@ -67,7 +69,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   if (wt >= WT) return;
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wc = wave % WC, part = wave / WC;
+  const int wc = wave % WC, wr = wave / WC % WR, part = wave / (WC * WR);
   const int rows = a.B * a.L, p_base = mt * RB * 32, d = a.d;
   const int tile = (wt * WC + wc) * NC;                  // first column tile (the layout is padded to whole workgroups)
   const int KB = (d + kBlockK - 1) / kBlockK;
@@ -88,19 +90,21 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
       load_lds16<false, 0>(from + static_cast<uint64_t>(i) * 1024, lane * 16, lds0 + K::BASE + K::TABLE + K::SUMS + i * 1024);
   }
   // ---- loads of a step: this wavefront's block of weights, its share of the h rows ---------------------------
-  const uint64_t wbase = reinterpret_cast<uint64_t>(q.codes) + static_cast<uint64_t>(tile) * KB * kBlockBytes;
+  const uint64_t wbase = reinterpret_cast<uint64_t>(q.codes) + static_cast<uint64_t>(wt) * K::COLTILES * KB * kBlockBytes;
   const int h0 = first_h_row(p_base, C, a.L);
   const uint64_t hbase = reinterpret_cast<uint64_t>(a.h) + static_cast<uint64_t>(h0) * d * 2;
-  int hpart[HL], hchunk[HL];
+  // the chunk that a lane loads into slot lane % 8 of its row; the rows of its pieces are 8 NW apart: one swizzle
+  const int hchunk = (lane & 7) ^ ((((K::HROWS > 8 ? wave & 1 : 0) * 8 + (lane >> 3)) >> 1) & 7);
+  int hpart[HL];
   uint32_t hoff[HL], hlds[HL];
 #pragma unroll
   for (int i = 0; i < HL; ++i) {
     const int piece = (wave + i * NW) % K::HI;           // (fewer pieces than wavefronts: some are loaded twice, alike)
     const int r = piece % (K::HROWS / 8) * 8 + (lane >> 3), blk = r / HRB;
     hpart[i] = piece / (K::HROWS / 8);
-    hchunk[i] = (lane & 7) ^ ((r >> 1) & 7);
     hoff[i] = static_cast<uint32_t>(h_row(min(p_base + (blk / C) * 32, rows - 1), r % HRB, blk % C, C, a.L, rows) - h0) *
-              static_cast<uint32_t>(d) * 2u;
+                  static_cast<uint32_t>(d) * 2u +
+              hchunk * 16;
     hlds[i] = lds0 + K::WB + piece * 1024;
   }
   // Every part walks its blocks cyclically from a start of the workgroup's own: rows of h are d * 2 bytes apart, and from one
@@ -115,23 +119,24 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     static_for<HL>([&](auto ii) {
       constexpr int i = decltype(ii)::value;
       const int kb = __builtin_amdgcn_readfirstlane(min(hfirst[i] + at, KB - 1));
-      uint32_t off = hoff[i] + hchunk[i] * 16;
-      if (nch && kb == KB - 1) off = hoff[i] + min(hchunk[i], nch - 1) * 16;
+      uint32_t off = hoff[i];
+      if (nch && kb == KB - 1) off -= max(hchunk - (nch - 1), 0) * 16;
       load_lds16<false, 0>(hbase + static_cast<uint32_t>(kb) * 128u, off, __builtin_amdgcn_readfirstlane(hlds[i]) + stage * K::STAGE);
     });
   };
   auto load_w = [&](int at, int stage) __attribute__((always_inline)) {
-    const uint64_t from = wbase + static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(min(kb0 + at, KB - 1))) * static_cast<uint64_t>(kBlockBytes);
-    static_for<NC>([&](auto c) {
-      constexpr int i = decltype(c)::value;
-      load_lds16<false, i * 1024>(from + static_cast<uint64_t>(i) * KB * kBlockBytes, lane * 16, lds0 + wave * (NC * 1024) + stage * K::STAGE);
+    static_for<WL>([&](auto ii) {
+      const int piece = (wave * WL + decltype(ii)::value) % K::WP;       // (more wavefronts than blocks: some are loaded twice, alike)
+      const int kb = __builtin_amdgcn_readfirstlane(min(first_block(piece / K::COLTILES) + at, KB - 1));
+      load_lds16<false, 0>(wbase + (static_cast<uint64_t>(piece % K::COLTILES) * KB + kb) * kBlockBytes, lane * 16,
+                           lds0 + piece * kBlockBytes + stage * K::STAGE);
     });
   };
   // the ragged block: chunks past the end are zeroed by the wavefront that loaded something in their place
   auto clear_ragged = [&](int at, int stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < HL; ++i)
-      if (hfirst[i] + at >= KB - 1 && hchunk[i] >= nch)
+      if (hfirst[i] + at >= KB - 1 && hchunk >= nch)
         *reinterpret_cast<u32x4*>(lds + (hlds[i] - lds0) + stage * K::STAGE + lane * 16) = u32x4{0u, 0u, 0u, 0u};
   };
 
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
       if (STEP == 4) {
         if ((lane & 7) == 0) to[0] = terms;
       } else {
-        if ((lane & 3) == 0) to[(hchunk[i] >> 2) * K::HROWS] = terms;
+        if ((lane & 3) == 0) to[(hchunk >> 2) * K::HROWS] = terms;
       }
     }
   };
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     g = kb * 2 / per_group;
     left = per_group - kb * 2 % per_group;
   };
-  const unsigned char* const hrows = lds + K::WB + part * (K::HROWS * 128) + ln % HRB * 128;
+  const unsigned char* const hrows = lds + K::WB + (part * K::HROWS + wr * NB * HRB + ln % HRB) * 128;
   const unsigned char* const scales = slab + wc * NC * q.groups * (kTileCols * esize) + ln * esize;
   uint32_t hslot[4];                                     // of the first block's rows; rows 8 apart differ in bit 2 of the swizzle
 #pragma unroll
@@ -192,10 +197,10 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   };
   auto fetch = [&](int parity, int stage, uint32_t keep, Operands& x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) x.w[c] = *reinterpret_cast<const u32x4*>(lds + stage * K::STAGE + (wave * NC + c) * 1024 + lane * 16);
+    for (int c = 0; c < NC; ++c) x.w[c] = *reinterpret_cast<const u32x4*>(lds + stage * K::STAGE + (part * K::COLTILES + wc * NC + c) * kBlockBytes + lane * 16);
 #pragma unroll
     for (int half = 0; half < PER; ++half) {
-      const uint2* const hs = hsum + ((parity * WK + part) * 2 + half) * K::HROWS + ln % HRB;
+      const uint2* const hs = hsum + ((parity * WK + part) * 2 + half) * K::HROWS + wr * NB * HRB + ln % HRB;
 #pragma unroll
       for (int i = 0; i < NB; ++i) x.rows[half][i] = hs[i * HRB];
 #pragma unroll
@@ -262,9 +267,9 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 
   // Step t.  Its barrier says that the wavefronts are done with step t - 1 and that step t + 1's rows and their sums are in LDS, whose
   // first operands are fetched under this step's MFMAs.  The rows of step t + S - 1 go to the stage of step t - 1, and the weights
-  // of step t + S to this wavefront's part of stage t, which it has in registers: they come from further away.  Late in the step
+  // of step t + S to stage t, whose weights are in registers: they come from further away.  Late in the step
   // the rows of step t + 2, loaded by then, are added up.
-  constexpr int MAY_FLY = (S - 3) * HL + (S - 2) * NC;   // loads issued behind the rows of step t + 2
+  constexpr int MAY_FLY = (S - 3) * HL + (S - 2) * WL;   // loads issued behind the rows and weights of step t + 2
   int h_ahead = rot, w_ahead = rot;                      // indices of the blocks to be loaded next
 #pragma unroll
   for (int t = 0; t < S; ++t) {
@@ -277,8 +282,8 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
       w_ahead = next_of(w_ahead);
     }
   }
-  // the rows of steps 0 and 1
-  if (S <= T) wait_loads<MAY_FLY + NC>();
+  // the rows and weights of steps 0 and 1
+  if (S <= T) wait_loads<MAY_FLY>();
   else wait_loads<0>();
   int now = rot, rows_at = rot;                          // indices of the blocks to be multiplied and to be added up next
 #pragma unroll
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     const int v = (tile + c) * kTileCols + ln;
     if (v >= a.n) continue;
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
+    for (int r = 0; r < RB / WR; ++r)
 #pragma unroll
       for (int ee = 0; ee < 16 / WK; ++ee) {
         // the wavefronts of a tile store a share of its elements each
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
           cond = uncond = 0.f;
 #pragma unroll
           for (int p = 0; p < WK; ++p) {
-            const float* const from = red + (((p * WC + wc) * NC + c) * NB + r * C) * 1024 + e * 64 + lane;
+            const float* const from = red + (((p * WC + wc) * NC + c) * NB + r * C) * 1024 + e * 64 + lane;      // (WR is 1)
             cond += from[0];
             uncond += from[(C - 1) * 1024];
           }
@@ -366,7 +371,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
           cond = sum[c][r * C][ee];
           uncond = sum[c][r * C + C - 1][ee];
         }
-        const int row = table[r * 32 + (e >> 2) * 8 + lg * 4 + (e & 3)];
+        const int row = table[(wr * (RB / WR) + r) * 32 + (e >> 2) * 8 + lg * 4 + (e & 3)];
         if (row >= 0) a.z[static_cast<int64_t>(row) * a.n + v] = processed_logit<C>(a, cond, uncond);
       }
   }
@@ -463,13 +468,19 @@ void launch_step(const LmHeadArgs& a, const QuantizedArgs& q, dim3 grid, int WT,
   if (q.zeros) hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, true>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
   else hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, false>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
 }
+// Two column tiles per wavefront leave no registers for groups that end inside a block: those have one.
+inline bool whole_blocks(const QuantizedArgs& q) { return q.group % kBlockK == 0; }
 template <class K>
 hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
   const int64_t tiles = up(a.n, kTileCols) / kTileCols;
   const int WT = static_cast<int>((tiles + K::COLTILES - 1) / K::COLTILES), MT = (a.B * a.L + K::RB * 32 - 1) / (K::RB * 32);
   const dim3 grid((WT + 7) / 8 * 8 * MT);
-  if (q.group % kBlockK == 0) launch_step<K, 4>(a, q, grid, WT, MT, s);
-  else launch_step<K, 2>(a, q, grid, WT, MT, s);
+  if constexpr (K::NC == 2) {
+    launch_step<K, 4>(a, q, grid, WT, MT, s);
+  } else {
+    if (whole_blocks(q)) launch_step<K, 4>(a, q, grid, WT, MT, s);
+    else launch_step<K, 2>(a, q, grid, WT, MT, s);
+  }
   return hipGetLastError();
 }
 static_assert(QuantCfg<2, 1, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4 && QuantCfg<1, 2, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4,
@@ -484,7 +495,7 @@ hipError_t launch_parts(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t
   using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
   using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
   using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
-  if (work >= 1536 && scales_fit<Wide>(q)) return launch<Wide>(a, q, s);
+  if (work >= 1536 && whole_blocks(q) && scales_fit<Wide>(q)) return launch<Wide>(a, q, s);
   if (work >= 1536 && scales_fit<One>(q)) return launch<One>(a, q, s);
   if (work >= 768 && scales_fit<Two>(q)) return launch<Two>(a, q, s);
   if constexpr (HRB == 8) {
@@ -492,6 +503,16 @@ hipError_t launch_parts(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t
     if (scales_fit<Small>(q)) return launch<Small>(a, q, s);
   }
   return launch<Four>(a, q, s);
+}
+
+// Many rows: 256 of h and 128 columns (64 where groups end inside blocks) per workgroup, a quarter of the rows per wavefront.
+// False: the scales do not fit.
+template <int C, int NC>
+bool try_tiles(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
+  using Tiles = QuantCfg<C, 8 / C, 32, NC, 8, 1, 160, 4>;
+  if (!scales_fit<Tiles>(q)) return false;
+  (void)launch<Tiles>(a, q, s);
+  return true;
 }
 
 }  // namespace
@@ -526,6 +547,11 @@ hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int
   q.scales = static_cast<const char*>(packed) + padded_tiles(a.n) * k_blocks(a.d) * kBlockBytes;
   q.group = group; q.groups = (a.d + group - 1) / group; q.zeros = zeros;
   const int rows = a.B * a.L;
+  if (rows > 128 / a.C) {
+    const bool done = a.C == 2 ? (whole_blocks(q) ? try_tiles<2, 2>(a, q, s) : try_tiles<2, 1>(a, q, s))
+                               : (whole_blocks(q) ? try_tiles<1, 2>(a, q, s) : try_tiles<1, 1>(a, q, s));
+    if (done) return hipGetLastError();
+  }
   if (a.C == 2) {
     if (rows <= 8) return launch_parts<2, 1, 8>(a, q, s);
     return launch_parts<2, 1, 32>(a, q, s);

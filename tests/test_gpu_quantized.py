@@ -56,7 +56,10 @@ CASES = [  # B, L, lam, V, v_lo, n, d, group, zeros, tau
     (1, 33, 0.0, 200, 0, 199, 1288, 64, True, 1.0), (3, 32, 3.0, 1000, 40, 900, 520, 32, False, 1.0), (1, 64, 0.0, 31, 0, 31, 4096, 256, True, 1.0),
     (5, 26, 0.0, 1285, 0, 1285, 1304, 1280, False, 1.0), (1, 32, 3.0, 33000, 3, 32900, 192, 64, True, 1.0),
     (1, 9, 0.0, 66000, 100, 65800, 72, 32, False, 1.0), (4, 40, 1.5, 34000, 0, 33333, 96, 96, True, 2.0), (1, 32, 3.0, 66000, 0, 66000, 1024, 32, True, 1.0),
-    (1, 2, 0.0, 70000, 0, 70000, 2048, 32, True, 1.0), (2, 17, 3.0, 260, 0, 256, 8192, 32, True, 1.0), (1, 60, 0.0, 65600, 9, 65555, 256, 160, False, 1.0)]
+    (1, 2, 0.0, 70000, 0, 70000, 2048, 32, True, 1.0), (2, 17, 3.0, 260, 0, 256, 8192, 32, True, 1.0), (1, 60, 0.0, 65600, 9, 65555, 256, 160, False, 1.0),
+    # many rows: tiles of 256 rows of h, by groups of whole and of half blocks, the last row tile ragged, and with scales that do not fit
+    (4, 33, 3.0, 700, 2, 645, 328, 64, True, 1.0), (9, 31, 3.0, 300, 0, 300, 136, 128, False, 0.8), (3, 64, 0.0, 515, 0, 500, 712, 192, True, 1.0),
+    (2, 150, 0.0, 200, 10, 130, 200, 32, False, 1.0), (1, 129, 0.0, 64, 0, 64, 64, 64, True, 1.0), (5, 30, 2.0, 260, 0, 259, 7000, 32, True, 1.0)]
 
 
 @pytest.mark.parametrize("Bn,L,lam,V,v_lo,n,d,group,zeros,tau", CASES)

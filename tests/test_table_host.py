@@ -90,3 +90,51 @@ def test_backward_workspace_does_not_hold_the_logits(rows, V, d):
         # a piece of 400 MiB or of 256 columns, the rows turned and their gradient's sums
         piece = max(400 << 20, 256 * 2 * (rows * 4 + d + 512))
         assert need <= piece * 1.1 + rows * d * 2 * 1.1 + 16 * 4 * rows * d + (1 << 20)
+
+
+def test_quantize_refuses():
+    c, p = Ctx(), ALIGNED
+    good = [c.ptr, p, 32, p, p, p]
+    _refused(c.lib.scd_quantize, good, [(0, None), (1, None), (2, 0), (2, -32), (2, 48), (3, None), (4, None), (1, p + 8), (3, p + 2),
+                                        (4, p + 1)])
+    good = [c.ptr, p, p, p, 32, p]
+    _refused(c.lib.scd_pack_quantized, good, [(0, None), (1, None), (2, None), (4, 0), (4, 40), (5, None), (1, p + 1), (2, p + 1), (5, p + 128)])
+    many = Ctx(d=32 * 257)                                  # 257 groups of 32, 129 of 64
+    assert c.lib.scd_quantize(many.ptr, p, 32, p, p, None) == B.SCD_EINVAL
+    bare = Ctx(d=0)
+    assert c.lib.scd_quantize(bare.ptr, p, 32, p, p, None) == B.SCD_EINVAL
+
+
+def test_quantized_bytes():
+    size = B.load().scd_quantized_bytes
+    bad = [(dict(d=64), 0, 0), (dict(d=64), 33, 0), (dict(d=64), 32, 2), (dict(d=64), 32, -1), (dict(d=0), 32, 0), (dict(d=32 * 257), 32, 0),
+           (dict(d=12), 32, 0)]
+    for kw, group, zeros in bad:
+        cfg = B.make_config(**dict(dict(B=1, L=1, N=1, V=100), **kw))
+        assert size(ctypes.byref(cfg), group, zeros) == 0, (kw, group, zeros)
+    # 4 bits a weight, padded to 256 columns and 64 weights, two or four bytes a group
+    cfg = B.make_config(B=1, L=1, N=1, V=5000, d=4096, v_lo=4, v_hi=4100)
+    assert 4096 * 2048 <= size(ctypes.byref(cfg), 64, 0) - 4096 * 64 * 2 <= 4096 * 2048 + 2048
+    assert 4096 * 2048 <= size(ctypes.byref(cfg), 64, 1) - 4096 * 64 * 4 <= 4096 * 2048 + 2048
+    assert size(ctypes.byref(B.make_config(B=1, L=1, N=1, V=5000, d=32 * 257)), 64, 0) > 0
+
+
+def test_lm_head_quantized_refuses():
+    c, p = Ctx(), ALIGNED
+    w = lambda at, group, zeros: ctypes.byref(B.ScdQuantized(at, group, zeros))  # noqa: E731
+    for call, align in ((c.lib.scd_lm_head_quantized, 4), (c.lib.scd_step_quantized, 256)):
+        good = [c.ptr, p, w(p, 32, 0), p]
+        _refused(call, good, [(0, None), (1, None), (2, None), (3, None), (1, p + 8), (3, p + align // 2), (2, w(None, 32, 0)), (2, w(p + 16, 32, 0)),
+                              (2, w(p, 0, 0)), (2, w(p, 16, 0)), (2, w(p, 32, 2))])
+        bare = Ctx(d=0)
+        assert call(bare.ptr, *good[1:]) == B.SCD_EINVAL
+
+
+def test_every_entry_point_of_the_header_is_exported_and_bound():
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(root, "include", "scd.h")).read(), flags=re.S)
+    lib = B.load()
+    for name in re.findall(r"\b(scd_\w+)\s*\(", text):
+        assert getattr(lib, name).argtypes is not None or name == "scd_strerror", name
