@@ -159,7 +159,7 @@ typedef enum scd_field {
 } scd_field;
 
 /* Bytes of caller-provided device scratch a context needs; 0 on a bad config.  Nothing in it outlives
- * a call.  scd_couple_draft writes it, and so do scd_select, scd_step and scd_step_logits where a
+ * a call.  scd_couple_draft writes it, and so do scd_select, scd_step, scd_step_quantized and scd_step_logits where a
  * top-k of up to 3072 filters rows of more than 16384 ids; those calls must not overlap in time on
  * the GPU with others that were given the same workspace. */
 size_t scd_workspace_bytes(const scd_config* cfg);
@@ -277,10 +277,10 @@ int scd_step_logits(scd_ctx* ctx, const float* d_z, void* d_state);
 
 /* ---- the LM head over 4-bit weights -----------------------------------------------------------
  *   W[v, k] = s[v, k / group] * (q[v, k] - o[v, k / group]),   q in 0..15, o = 8, or a zero point of 0..15.
- * group: weights of a row that share a scale, a positive multiple of 32 (the last group of a row may be shorter), at most 256
+ * group: weights of a row that share a scale, a multiple of 32 up to 65536 (the last group of a row may be shorter), at most 256
  * groups per row.  Row-major arrays, as a checkpoint holds them: d_codes uint8 [V, d / 2], even k in the low half of a
  * byte (4-byte aligned); d_scales bf16 [V, G] and d_zeros uint8 [V, G] (NULL: o = 8), G = ceil(d / group).  The steps read
- * them in another layout, made once by scd_pack_quantized.  All need cfg.d > 0. */
+ * them in another layout, made once by scd_pack_quantized.  All need cfg.d in 8 .. 2^20. */
 typedef struct scd_quantized {
   const void* d_packed;   /* written by scd_pack_quantized for this configuration's allowed ids and d */
   int32_t group;
@@ -307,9 +307,9 @@ int scd_step_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W
 
 /* ---- the vocabulary table at the model's other end, and what it learns -------------------------
  * The same table W, bf16 bits [V, d] row-major, all pointers 16-byte aligned (d_ids, d_targets and the
- * float arrays 4-byte).  All of them need cfg.d > 0; of the rest of the configuration they use what is
+ * float arrays 4-byte).  All of them need cfg.d > 0 (up to 2^24); of the rest of the configuration they use what is
  * named below, so a context with B = L = N = 1 serves a program that decodes nothing.  `rows` = 0 is allowed (arrays of
- * no elements may then be NULL).  Workspaces are the caller's, 256-byte aligned, of the size that the
+ * no elements may then be NULL), up to 2^25 ids or 2^20 rows of the loss.  Workspaces are the caller's, 256-byte aligned, of the size that the
  * query gives for the same arguments (0 for bad ones); nothing in one outlives the call.  Calls on different
  * streams, contexts or in different recorded graphs must not share one if they may overlap in time. */
 
@@ -341,7 +341,8 @@ int scd_embed_backward(scd_ctx* ctx, const int32_t* d_ids, int32_t rows, const u
  * top_k, top_p and the decode options do not enter; cfg_lambda must be 0 (SCD_EUNSUPPORTED otherwise).
  *   d_h bf16 [rows, d];  d_targets int32 [rows], OFFSETS into the allowed ids; a negative one leaves the row out (loss 0,
  * no gradient, whatever the row holds), one of n or more is not an allowed id (loss +inf, gradient of the normaliser alone);
- *   d_loss, d_lse fp32 [rows], written.  rows up to 2^20. */
+ *   d_loss, d_lse fp32 [rows], written.  rows * allowed ids up to 2^38, d up to 2^21
+ * (SCD_EUNSUPPORTED beyond). */
 size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows);
 int scd_cross_entropy(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
                       float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes);

@@ -8,7 +8,10 @@
 // wavefront walks a chunk of the sorted rows along 512 columns.  An id whose rows lie in one chunk is done there; one
 // that reaches over a chunk's border leaves a partial sum per chunk, and join_kernel adds those up, in order, by several
 // wavefronts: one id may hold most of the rows.  Ids that no row has get their zeros in the same launch as the sums,
-// from workgroups that look their stretch of ids up in the sorted list.
+// from workgroups behind them that look their stretch of ids up in the sorted list.
+//   Bound by memory where there is much to move: 25600 rows of 4096 (a fifth in one id) on 64000 ids take 189 us, 150 of them in the sums'
+// launch (4.9 TB/s), 31 for sorting and 7.5 for joining; by its three launches where there is not (576 rows of 1280 on 16384 ids, fp32: 33 us,
+// 16 of them the zeros' bytes).  The lookup of 25600 rows takes 66 us, of 64 rows 5.4, a launch.
 #include "scd_device.h"
 #include "scd_kernels.h"
 
@@ -43,7 +46,7 @@ __device__ __forceinline__ void embed_row(const u32x4* __restrict__ W, int64_t i
 
 __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ ids, const u32x4* __restrict__ W, u32x4* __restrict__ x,
                                                     int rows, int V, int d8, float scale) {
-  const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // up to 2^25 rows: in range
   if (r >= rows) return;
   const int id = ids[r];
   embed_row(W, id, id >= 0 && id < V, d8, blockIdx.y * (64 * kPieces), scale, x + static_cast<int64_t>(r) * d8);
@@ -53,10 +56,10 @@ __global__ __launch_bounds__(256) void embed_kernel(const int32_t* __restrict__ 
 __global__ __launch_bounds__(256) void embed_window_kernel(const EmbedArgs a) {
   const int r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (r >= a.rows) return;
-  const int s = r % a.L, b = r / a.L / a.C, left = a.N - a.pos[b];
-  const int slot = s < left ? (a.pos[b] + s) % a.L : 0;
-  const int id = a.v_lo + a.X[static_cast<int64_t>(b) * a.L + slot];
-  embed_row(reinterpret_cast<const u32x4*>(a.W), id, s < left && id >= 0 && id < a.V, a.d / 8, blockIdx.y * (64 * kPieces), a.scale,
+  const int s = r % a.L, b = r / a.L / a.C, pos = a.pos[b];
+  const bool live = pos >= 0 && s < a.N - pos;
+  const int id = a.v_lo + a.X[static_cast<int64_t>(b) * a.L + (live ? (pos + s) % a.L : 0)];
+  embed_row(reinterpret_cast<const u32x4*>(a.W), id, live && id >= 0 && id < a.V, a.d / 8, blockIdx.y * (64 * kPieces), a.scale,
             reinterpret_cast<u32x4*>(a.x) + static_cast<int64_t>(r) * (a.d / 8));
 }
 
@@ -273,6 +276,7 @@ __global__ __launch_bounds__(kWaves * 64) void sort_move_kernel(const int32_t* _
 
 // ---- sums ----------------------------------------------------------------------------------------
 constexpr int kSlice = 512;      // columns of a wavefront: 8 per lane
+constexpr uint32_t kZeroIds = 16;
 
 // dW row `id`, this lane's 8 columns from `col`: one rounding
 template <bool F32, bool ACC>
@@ -299,8 +303,8 @@ struct SumArgs {
   const uint16_t* dx;
   void* dW;
   float* part;          // [chunks][2][d]: sums of the chunk's first id (it began before the chunk) and of its last (it goes on)
-  int rows, V, d, chunk, chunks, zero_blocks, zero_ids;
-  uint32_t sum_blocks;
+  int rows, V, d, chunk, chunks;
+  uint32_t sum_blocks, zero_blocks;
   float scale;
 };
 
@@ -312,33 +316,36 @@ template <bool F32, bool ACC>
 __global__ __launch_bounds__(256) void sum_kernel(const SumArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (!ACC && blockIdx.x >= a.sum_blocks) {
-    // ---- rows that no id has: a workgroup looks after zero_ids neighbouring ids of dW --------------------
-    __shared__ uint32_t seen[kMaxBins];
-    const uint32_t v0 = (blockIdx.x - a.sum_blocks) * a.zero_ids, v1 = min(v0 + a.zero_ids, static_cast<uint32_t>(a.V));
-    for (int i = threadIdx.x; i < a.zero_ids; i += 256) seen[i] = 0u;
-    __syncthreads();
-    // the first sorted row with a key of v0 or more, 64 places at a time
-    int64_t lo = 0, hi = a.rows;         // in [lo, hi]
-    while (hi > lo) {
-      const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-      const bool below = at < hi && a.sorted[at].key < v0;
-      const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
-      if (n == 0) hi = lo;
-      else {
-        hi = min(hi, lo + n * step);
-        lo = lo + (n - 1) * step + 1;
+    // ---- rows that no id has: a workgroup looks after kZeroIds neighbouring ids of dW at a time --------------------
+    __shared__ uint32_t seen[kZeroIds];
+    for (uint32_t stretch = blockIdx.x - a.sum_blocks; stretch < (a.V - 1u) / kZeroIds + 1u; stretch += a.zero_blocks) {
+      const uint32_t v0 = stretch * kZeroIds, v1 = min(v0 + kZeroIds, static_cast<uint32_t>(a.V));
+      __syncthreads();
+      if (threadIdx.x < kZeroIds) seen[threadIdx.x] = 0u;
+      __syncthreads();
+      // the first sorted row with a key of v0 or more, 64 places at a time
+      int64_t lo = 0, hi = a.rows;         // in [lo, hi]
+      while (hi > lo) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const bool below = at < hi && a.sorted[at].key < v0;
+        const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
+        if (n == 0) hi = lo;
+        else {
+          hi = min(hi, lo + n * step);
+          lo = lo + (n - 1) * step + 1;
+        }
       }
-    }
-    for (int64_t at = lo + threadIdx.x; at < a.rows; at += 256) {
-      const uint32_t key = a.sorted[at].key;
-      if (key >= v1) break;
-      seen[key - v0] = 1u;
-    }
-    __syncthreads();
-    const f32x8 zero{};
-    for (uint32_t v = v0 + wave; v < v1; v += 4) {
-      if (seen[v - v0]) continue;
-      for (int col = lane * 8; col < a.d; col += kSlice) put<F32, false>(a.dW, v, a.d, col, zero);
+      for (int64_t at = lo + threadIdx.x; at < a.rows; at += 256) {
+        const uint32_t key = a.sorted[at].key;
+        if (key >= v1) break;
+        seen[key - v0] = 1u;
+      }
+      __syncthreads();
+      const f32x8 zero{};
+      for (uint32_t v = v0 + wave; v < v1; v += 4) {
+        if (seen[v - v0]) continue;
+        for (int col = lane * 8; col < a.d; col += kSlice) put<F32, false>(a.dW, v, a.d, col, zero);
+      }
     }
     return;
   }
@@ -439,7 +446,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(const SumArgs a) 
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-// sorted rows of a wavefront
+// Sorted rows of a wavefront: more of them leave fewer partial sums of frequent ids to be joined (25600 rows of 4096, a fifth in one id: chunks
+// of 32 join in 14 - 19 us, of 64 in 7.5, and the sums take as long), fewer of them fill the chip when there are few rows.
 inline int chunk_rows(int rows) { return rows > (1 << 16) ? 128 : rows > (1 << 14) ? 64 : 32; }
 
 template <bool F32, bool ACC>
@@ -512,8 +520,7 @@ hipError_t launch_embed_backward(const EmbedBackwardArgs& e, hipStream_t s) {
     }
   }
   a.sorted = sorted;
-  a.zero_ids = 16;
-  a.zero_blocks = (e.V + a.zero_ids - 1) / a.zero_ids;
+  a.zero_blocks = min((e.V - 1u) / kZeroIds + 1u, 1u << 18);
   if (e.f32) return e.accumulate ? launch_sums<true, true>(a, s) : launch_sums<true, false>(a, s);
   return e.accumulate ? launch_sums<false, true>(a, s) : launch_sums<false, false>(a, s);
 }

@@ -34,7 +34,7 @@ struct TileOperand {
 
 // acc += the k-tiles kt0 .. kt0 + KT - 1, walked cyclically from the `rot`-th of them, and `tail` (< 64, a multiple of 8)
 // elements of the one behind.
-//   * W and h tiles of 128 bytes per row go straight into LDS; lane l of a load writes slot l % 8 of row l / 8 and reads
+//   * Tiles of 128 bytes per row go straight into LDS; lane l of a load writes slot l % 8 of row l / 8 and reads
 //     chunk (l % 8) ^ ((row >> 1) & 7): operand reads are then free of bank conflicts without padding.
 //   * One barrier per k-tile, in the middle of its last k-step: when it is passed the next tile is in LDS, its first
 //     operands are read under the last MFMAs of this one, and the stage just read is free.

@@ -17,9 +17,11 @@
 //
 // A workgroup of NW wavefronts owns NC * NW / (WK * WR) neighbouring column tiles, NC per wavefront; WK wavefronts share tiles and
 // rows and take 1/WK of k each (their sums are added up at the end in a fixed order), WR share tiles and take a part of the rows
-// each.  Weights and h rows go from memory straight into
-// LDS, S stages deep; a wavefront reads its own weights back, the h rows are shared.  The scales of the workgroup's columns are
-// fetched whole at the start.
+// each.  Weights and h rows go from memory straight into LDS, S stages deep.  The scales of the workgroup's columns are fetched whole at
+// the start.
+//   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096 take 56 us, of which the loads alone would take 25 to 30 (142 MB); a
+// wavefront issues about 220 vector instructions per step of two tiles (64 convert codes, 64 scale, 30 add rows up) beside 20 MFMAs, and the
+// matrix pipes are busy a quarter of the time.  With the offsets taken off by a product with ones it took 75, as C operands from LDS 63.
 #include "lm_head_rows.h"
 #include "tile_loads.h"
 
@@ -33,7 +35,7 @@ template <int C_, int RB_, int HRB_, int NC_, int NW_, int WK_, int KB_, int WR_
 struct QuantCfg {
   static constexpr int C = C_, RB = RB_, HRB = HRB_, NC = NC_, NW = NW_, WK = WK_, WR = WR_, LDS = KB_ * 1024;
   static constexpr int THREADS = NW * 64, WC = NW / WK / WR, COLTILES = WC * NC, NB = RB * C / WR;
-  static constexpr int HROWS = RB * C * HRB;                 // h rows per part of k
+  static constexpr int HROWS = RB * C * HRB;             // h rows per part of k
   static constexpr int HI = WK * HROWS / 8;              // load instructions for the h rows of a step, all parts
   static constexpr int HL = (HI + NW - 1) / NW;          // per wavefront
   static constexpr int WP = COLTILES * WK, WL = (WP + NW - 1) / NW;      // blocks of weights of a step, per wavefront to be loaded
@@ -59,7 +61,8 @@ __device__ __forceinline__ u32x4 codes_to_bf16(uint32_t w) {
 // STEP: MFMAs between two applications of a scale (2: groups that end inside a block of k, 4: they do not)
 template <class K, int STEP, bool ZEROS>
 __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmHeadArgs a, const QuantizedArgs q, const int WT, const int MT) {
-  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, WL = K::WL, WR = K::WR, WK = K::WK, WC = K::WC, NW = K::NW, S = K::S, HL = K::HL, HRB = K::HRB;
+  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, WL = K::WL, WR = K::WR, WK = K::WK, WC = K::WC, NW = K::NW;
+  constexpr int S = K::S, HL = K::HL, HRB = K::HRB;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[K::LDS];
   int* const table = reinterpret_cast<int*>(lds + K::BASE);
   uint2* const hsum = reinterpret_cast<uint2*>(lds + K::BASE + K::TABLE);     // [2][WK][2][HROWS]
@@ -95,11 +98,15 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   const uint64_t hbase = reinterpret_cast<uint64_t>(a.h) + static_cast<uint64_t>(h0) * d * 2;
   // the chunk that a lane loads into slot lane % 8 of its row; the rows of its pieces are 8 NW apart: one swizzle
   const int hchunk = (lane & 7) ^ ((((K::HROWS > 8 ? wave & 1 : 0) * 8 + (lane >> 3)) >> 1) & 7);
+  // Fewer pieces of h rows than wavefronts: the others load weights alone.  (Two that loaded a piece alike would not do: the one might clear
+  // the end of a ragged block and add its rows up while the other's load is still to land.)
+  const bool loads_h = K::HI >= NW || wave < K::HI;
+  static_assert(K::HI < NW || K::HI % NW == 0, "pieces per wavefront");
   int hpart[HL];
   uint32_t hoff[HL], hlds[HL];
 #pragma unroll
   for (int i = 0; i < HL; ++i) {
-    const int piece = (wave + i * NW) % K::HI;           // (fewer pieces than wavefronts: some are loaded twice, alike)
+    const int piece = (wave + i * NW) % K::HI;
     const int r = piece % (K::HROWS / 8) * 8 + (lane >> 3), blk = r / HRB;
     hpart[i] = piece / (K::HROWS / 8);
     hoff[i] = static_cast<uint32_t>(h_row(min(p_base + (blk / C) * 32, rows - 1), r % HRB, blk % C, C, a.L, rows) - h0) *
@@ -116,6 +123,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 #pragma unroll
   for (int i = 0; i < HL; ++i) hfirst[i] = first_block(hpart[i]);
   auto load_h = [&](int at, int stage) __attribute__((always_inline)) {
+    if (!loads_h) return;
     static_for<HL>([&](auto ii) {
       constexpr int i = decltype(ii)::value;
       const int kb = __builtin_amdgcn_readfirstlane(min(hfirst[i] + at, KB - 1));
@@ -134,6 +142,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   };
   // the ragged block: chunks past the end are zeroed by the wavefront that loaded something in their place
   auto clear_ragged = [&](int at, int stage) __attribute__((always_inline)) {
+    if (!loads_h) return;
 #pragma unroll
     for (int i = 0; i < HL; ++i)
       if (hfirst[i] + at >= KB - 1 && hchunk >= nch)
@@ -142,6 +151,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 
   // Sums of the h rows that this wavefront loaded: 8 lanes hold a row's block of k, 4 a half.
   auto add_rows = [&](int parity, int stage) __attribute__((always_inline)) {
+    if (!loads_h) return;
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
 #pragma unroll
@@ -269,7 +279,11 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   // first operands are fetched under this step's MFMAs.  The rows of step t + S - 1 go to the stage of step t - 1, and the weights
   // of step t + S to stage t, whose weights are in registers: they come from further away.  Late in the step
   // the rows of step t + 2, loaded by then, are added up.
-  constexpr int MAY_FLY = (S - 3) * HL + (S - 2) * WL;   // loads issued behind the rows and weights of step t + 2
+  // all loads issued by step t but those behind the rows and weights of step t + 2
+  auto wait_early_loads = [&]() __attribute__((always_inline)) {
+    if (loads_h) wait_loads<(S - 3) * HL + (S - 2) * WL>();
+    else wait_loads<(S - 2) * WL>();
+  };
   int h_ahead = rot, w_ahead = rot;                      // indices of the blocks to be loaded next
 #pragma unroll
   for (int t = 0; t < S; ++t) {
@@ -283,7 +297,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     }
   }
   // the rows and weights of steps 0 and 1
-  if (S <= T) wait_loads<MAY_FLY>();
+  if (S <= T) wait_early_loads();
   else wait_loads<0>();
   int now = rot, rows_at = rot;                          // indices of the blocks to be multiplied and to be added up next
 #pragma unroll
@@ -320,7 +334,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     fetch(1 - ODD, one, keep(then), x[1 - ODD]);         // (behind the last step: something that nobody uses)
     compute(x[ODD], stage, [&]() __attribute__((always_inline)) {
       if (t + 2 >= T) return;
-      if (t + S < T) wait_loads<MAY_FLY>();
+      if (t + S < T) wait_early_loads();
       else wait_loads<0>();
       if (nch) clear_ragged(rows_at, two);
       add_rows(ODD, two);
@@ -382,38 +396,38 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 // smallest) / 15 over a range that holds 0; s is rounded to bf16 first, the codes are the nearest under the rounded one.
 __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restrict__ W, int64_t items, int d, int group, int groups,
                                                        uint8_t* __restrict__ codes, uint16_t* __restrict__ scales, uint8_t* __restrict__ zeros) {
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (item >= items) return;
-  const int64_t v = item / groups;
-  const int g = static_cast<int>(item - v * groups), k0 = g * group, k1 = min(k0 + group, d);
-  const uint32_t* const row = reinterpret_cast<const uint32_t*>(W + v * d);       // two weights each
-  float lo = 0.f, hi = 0.f;
-  for (int k = k0 / 2 + lane; k < k1 / 2; k += 64) {
-    const uint32_t two = row[k];
-    const float x = __uint_as_float(two << 16), y = __uint_as_float(two & 0xFFFF0000u);
-    lo = fminf(lo, fminf(x, y));
-    hi = fmaxf(hi, fmaxf(x, y));
-  }
+  for (int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); item < items; item += static_cast<int64_t>(gridDim.x) * 4) {
+    const int64_t v = item / groups;
+    const int g = static_cast<int>(item - v * groups), k0 = g * group, k1 = min(k0 + group, d);
+    const uint32_t* const row = reinterpret_cast<const uint32_t*>(W + v * d);       // two weights each
+    float lo = 0.f, hi = 0.f;
+    for (int k = k0 / 2 + lane; k < k1 / 2; k += 64) {
+      const uint32_t two = row[k];
+      const float x = __uint_as_float(two << 16), y = __uint_as_float(two & 0xFFFF0000u);
+      lo = fminf(lo, fminf(x, y));
+      hi = fmaxf(hi, fmaxf(x, y));
+    }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor(lo, o, 64));
-    hi = fmaxf(hi, __shfl_xor(hi, o, 64));
-  }
-  const __bf16 sb = static_cast<__bf16>(zeros ? __fdiv_rn(hi - lo, 15.f) : fmaxf(__fdiv_rn(hi, 7.f), __fdiv_rn(-lo, 8.f)));
-  const float s = static_cast<float>(sb);
-  const int zero = zeros && s > 0.f ? static_cast<int>(fminf(rintf(__fdiv_rn(-lo, s)), 15.f)) : 8;
-  auto code = [&](float x) {
-    return s > 0.f ? static_cast<uint32_t>(fminf(fmaxf(rintf(__fdiv_rn(x, s)) + static_cast<float>(zero), 0.f), 15.f))
-                   : static_cast<uint32_t>(zero);
-  };
-  for (int k = k0 / 2 + lane; k < k1 / 2; k += 64) {
-    const uint32_t two = row[k];
-    codes[v * (d / 2) + k] = static_cast<uint8_t>(code(__uint_as_float(two << 16)) | code(__uint_as_float(two & 0xFFFF0000u)) << 4);
-  }
-  if (lane == 0) {
-    scales[item] = __builtin_bit_cast(uint16_t, sb);
-    if (zeros) zeros[item] = static_cast<uint8_t>(zero);
+    for (int o = 32; o > 0; o >>= 1) {
+      lo = fminf(lo, __shfl_xor(lo, o, 64));
+      hi = fmaxf(hi, __shfl_xor(hi, o, 64));
+    }
+    const __bf16 sb = static_cast<__bf16>(zeros ? __fdiv_rn(hi - lo, 15.f) : fmaxf(__fdiv_rn(hi, 7.f), __fdiv_rn(-lo, 8.f)));
+    const float s = static_cast<float>(sb);
+    const int zero = zeros && s > 0.f ? static_cast<int>(fminf(rintf(__fdiv_rn(-lo, s)), 15.f)) : 8;
+    auto code = [&](float x) {
+      return s > 0.f ? static_cast<uint32_t>(fminf(fmaxf(rintf(__fdiv_rn(x, s)) + static_cast<float>(zero), 0.f), 15.f))
+                     : static_cast<uint32_t>(zero);
+    };
+    for (int k = k0 / 2 + lane; k < k1 / 2; k += 64) {
+      const uint32_t two = row[k];
+      codes[v * (d / 2) + k] = static_cast<uint8_t>(code(__uint_as_float(two << 16)) | code(__uint_as_float(two & 0xFFFF0000u)) << 4);
+    }
+    if (lane == 0) {
+      scales[item] = __builtin_bit_cast(uint16_t, sb);
+      if (zeros) zeros[item] = static_cast<uint8_t>(zero);
+    }
   }
 }
 
@@ -441,20 +455,22 @@ __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t* __restri
 }
 __global__ __launch_bounds__(256) void pack_scales_kernel(const uint16_t* __restrict__ scales, const uint8_t* __restrict__ zeros, int n, int groups,
                                                           int64_t count, void* __restrict__ to) {
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;        // (tile, group, column)
-  if (at >= count) return;
-  const int64_t tile = at / (static_cast<int64_t>(groups) * kTileCols), v = tile * kTileCols + at % kTileCols;
-  const int64_t from = v * groups + at / kTileCols % groups;
-  const uint32_t s = v < n ? scales[from] : 0u;
-  if (zeros) {
-    const float o = 16.f + (v < n ? static_cast<float>(min(static_cast<int>(zeros[from]), 15)) : 0.f);
-    static_cast<uint32_t*>(to)[at] = s | (__float_as_uint(o) & 0xFFFF0000u);        // exact: o has five bits
-  } else {
-    static_cast<uint16_t*>(to)[at] = static_cast<uint16_t>(s);
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < count; at += static_cast<int64_t>(gridDim.x) * 256) {
+    // at: (tile, group, column)
+    const int64_t tile = at / (static_cast<int64_t>(groups) * kTileCols), v = tile * kTileCols + at % kTileCols;
+    const int64_t from = v * groups + at / kTileCols % groups;
+    const uint32_t s = v < n ? scales[from] : 0u;
+    if (zeros) {
+      const float o = 16.f + (v < n ? static_cast<float>(min(static_cast<int>(zeros[from]), 15)) : 0.f);
+      static_cast<uint32_t*>(to)[at] = s | (__float_as_uint(o) & 0xFFFF0000u);        // exact: o has five bits
+    } else {
+      static_cast<uint16_t*>(to)[at] = static_cast<uint16_t>(s);
+    }
   }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------
+constexpr int64_t kMostBlocks = 1 << 20;      // of kernels that loop over what is left
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 inline int64_t padded_tiles(int n) { return up(up(n, kTileCols) / kTileCols, kTilesPad); }
 inline int k_blocks(int d) { return (d + kBlockK - 1) / kBlockK; }
@@ -525,7 +541,7 @@ size_t quantized_bytes(int n, int d, int group, bool zeros) {
 hipError_t launch_quantize(const uint16_t* W, int V, int d, int group, uint8_t* codes, uint16_t* scales, uint8_t* zeros, hipStream_t s) {
   const int groups = (d + group - 1) / group;
   const int64_t items = static_cast<int64_t>(V) * groups;
-  hipLaunchKernelGGL(quantize_kernel, dim3(static_cast<uint32_t>((items + 3) / 4)), dim3(256), 0, s, W, items, d, group, groups, codes, scales, zeros);
+  hipLaunchKernelGGL(quantize_kernel, dim3(static_cast<uint32_t>((items + 3) / 4 < kMostBlocks ? (items + 3) / 4 : kMostBlocks)), dim3(256), 0, s, W, items, d, group, groups, codes, scales, zeros);
   return hipGetLastError();
 }
 
@@ -536,7 +552,7 @@ hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, c
   hipLaunchKernelGGL(pack_codes_kernel, dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s, codes, n, d, k_blocks(d), blocks,
                      static_cast<u32x4*>(packed));
   const int64_t count = tiles * groups * kTileCols;
-  hipLaunchKernelGGL(pack_scales_kernel, dim3(static_cast<uint32_t>((count + 255) / 256)), dim3(256), 0, s, scales, zeros, n, groups, count,
+  hipLaunchKernelGGL(pack_scales_kernel, dim3(static_cast<uint32_t>((count + 255) / 256 < kMostBlocks ? (count + 255) / 256 : kMostBlocks)), dim3(256), 0, s, scales, zeros, n, groups, count,
                      static_cast<char*>(packed) + blocks * kBlockBytes);
   return hipGetLastError();
 }

@@ -356,8 +356,20 @@ int couple_draft_impl(scd_ctx* c, char* w, bool cands, const float* d_z_cur, con
   return hip_rc(scd::launch_row(ra, c->stream, c->row_lds));
 }
 
+// What the operators on the vocabulary table check alike.
+constexpr int32_t kCrossEntropyRows = 1 << 20, kEmbedRows = 1 << 25, kEmbedWidth = 1 << 24, kMostIds = 1 << 30;
+inline bool cross_entropy_fits(int32_t rows, int32_t n, int32_t d) {      // tiles that one launch can hold, rows that 32 bits reach
+  return n <= kMostIds && d <= (1 << 21) && static_cast<int64_t>(rows) * n <= static_cast<int64_t>(1) << 38;
+}
+inline bool valid_gradient(int32_t grad_type, int32_t accumulate) {
+  return (grad_type == SCD_GRAD_BF16 || grad_type == SCD_GRAD_F32) && (accumulate == 0 || accumulate == 1);
+}
+inline bool valid_workspace(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
+
 bool valid_group(const scd_config& c, int32_t group) {
-  return c.d > 0 && group > 0 && group % 32 == 0 && (static_cast<int64_t>(c.d) + group - 1) / group <= scd::kMaxGroups;
+  // (the kernel's offsets into the rows that a workgroup reads have 32 bits)
+  return c.d > 0 && c.d <= (1 << 20) && c.v_hi - c.v_lo <= kMostIds && group > 0 && group <= 65536 && group % 32 == 0 &&
+         (static_cast<int64_t>(c.d) + group - 1) / group <= scd::kMaxGroups;
 }
 int quantized_args(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, scd::LmHeadArgs* a) {
   if (!c || !d_h || !W || !W->d_packed || !aligned(d_h, 16) || !aligned(W->d_packed, kAlign)) return SCD_EINVAL;
@@ -370,18 +382,11 @@ int quantized_args(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, scd:
   return SCD_OK;
 }
 
-// What the operators on the vocabulary table check alike.
-constexpr int32_t kCrossEntropyRows = 1 << 20;
-inline bool valid_gradient(int32_t grad_type, int32_t accumulate) {
-  return (grad_type == SCD_GRAD_BF16 || grad_type == SCD_GRAD_F32) && (accumulate == 0 || accumulate == 1);
-}
-inline bool valid_workspace(const void* ws, size_t bytes, size_t need) { return ws && aligned(ws, kAlign) && bytes >= need; }
-
 int cross_entropy_args(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
                        scd::CrossEntropyArgs* a) {
   if (!d_W || rows < 0 || rows > kCrossEntropyRows || (rows > 0 && (!d_h || !d_targets)) || c->cfg.d <= 0) return SCD_EINVAL;
   if (!aligned(d_h, 16) || !aligned(d_W, 16) || !aligned(d_targets, 4)) return SCD_EINVAL;
-  if (c->C != 1) return SCD_EUNSUPPORTED;
+  if (c->C != 1 || !cross_entropy_fits(rows, c->n, c->cfg.d)) return SCD_EUNSUPPORTED;
   a->h = d_h;
   a->W = d_W + static_cast<size_t>(c->cfg.v_lo) * c->cfg.d;
   a->targets = d_targets;
@@ -549,12 +554,13 @@ int scd_step_quantized(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, 
 
 // ---- operators on the vocabulary table ---------------------------------------------------
 size_t scd_embed_backward_workspace_bytes(const scd_config* cfg, int32_t rows) {
-  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0) return 0;
+  if (!valid_config(cfg) || cfg->d <= 0 || cfg->d > kEmbedWidth || rows < 0 || rows > kEmbedRows) return 0;
   return scd::embed_backward_bytes(rows, cfg->d);
 }
 
 int scd_embed(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uint16_t* d_W, float scale, uint16_t* d_x) {
-  if (!c || !d_W || rows < 0 || (rows > 0 && (!d_ids || !d_x)) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!c || !d_W || rows < 0 || rows > kEmbedRows || (rows > 0 && (!d_ids || !d_x)) || c->cfg.d <= 0 || c->cfg.d > kEmbedWidth)
+    return SCD_EINVAL;
   if (!aligned(d_ids, 4) || !aligned(d_W, 16) || !aligned(d_x, 16)) return SCD_EINVAL;
   scd::EmbedArgs a{};
   a.ids = d_ids; a.W = d_W; a.x = d_x;
@@ -563,10 +569,10 @@ int scd_embed(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uint16_t* d_
 }
 
 int scd_embed_window(scd_ctx* c, const void* d_state, const uint16_t* d_W, float scale, uint16_t* d_x) {
-  if (!c || !d_state || !d_W || !d_x || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!c || !d_state || !d_W || !d_x || c->cfg.d <= 0 || c->cfg.d > kEmbedWidth) return SCD_EINVAL;
   if (!aligned(d_state, kAlign) || !aligned(d_W, 16) || !aligned(d_x, 16)) return SCD_EINVAL;
   const int64_t rows = static_cast<int64_t>(c->cfg.B) * c->C * c->cfg.L;
-  if (rows > INT32_MAX) return SCD_EUNSUPPORTED;
+  if (rows > kEmbedRows) return SCD_EUNSUPPORTED;
   void* const st = const_cast<void*>(d_state);
   scd::EmbedArgs a{};
   a.W = d_W; a.x = d_x;
@@ -579,7 +585,8 @@ int scd_embed_window(scd_ctx* c, const void* d_state, const uint16_t* d_W, float
 
 int scd_embed_backward(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uint16_t* d_dx, float scale, void* d_dW,
                        int32_t grad_type, int32_t accumulate, void* d_workspace, size_t workspace_bytes) {
-  if (!c || !d_dW || rows < 0 || (rows > 0 && (!d_ids || !d_dx)) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!c || !d_dW || rows < 0 || rows > kEmbedRows || (rows > 0 && (!d_ids || !d_dx)) || c->cfg.d <= 0 || c->cfg.d > kEmbedWidth)
+    return SCD_EINVAL;
   if (!valid_gradient(grad_type, accumulate)) return SCD_EINVAL;
   if (!aligned(d_ids, 4) || !aligned(d_dx, 16) || !aligned(d_dW, 16)) return SCD_EINVAL;
   if (!valid_workspace(d_workspace, workspace_bytes, scd::embed_backward_bytes(rows, c->cfg.d))) return SCD_EWORKSPACE;
@@ -592,12 +599,14 @@ int scd_embed_backward(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uin
 }
 
 size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows) {
-  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows) return 0;
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d)) return 0;
   return scd::cross_entropy_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d);
 }
 
 size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type) {
-  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !valid_gradient(grad_type, 0)) return 0;
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !valid_gradient(grad_type, 0) ||
+      !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d))
+    return 0;
   return scd::cross_entropy_backward_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d, grad_type == SCD_GRAD_F32);
 }
 
