@@ -20,6 +20,7 @@ struct GemmTile {
   static constexpr int AB = HR * 128, BB = BN * 128;          // bytes per stage
   static constexpr int SB = 3, SA = HR == 256 && BN > 128 ? 2 : 3;
   static constexpr int STAGES = SB * BB + SA * AB;
+  static constexpr int kChain = 8;                            // k-tiles that a running sum holds where sums are folded
   static_assert(WCOL * WROW == NW && WROW * RW == HR && WCOL * CW == BN && AL * NW * 8 == HR && BL * NW * 8 == BN && STAGES <= 160 * 1024, "tile shape");
 };
 
@@ -40,8 +41,10 @@ struct TileOperand {
 //     operands are read under the last MFMAs of this one, and the stage just read is free.
 //   * Loads are issued one by one between MFMAs: eight wavefronts issuing all of theirs after the barrier would queue at
 //     the one address unit with their MFMAs behind them.
+// FOLDS: running sums go into whole ones every kChain k-tiles and start again, since one chain of 32-bit additions over k
+// errs with its length; in the registers that small tiles have left.
 // Ends with loads, MFMAs' operands and stages all settled for this wavefront; a barrier has to follow before LDS is reused.
-template <class K, bool F16>
+template <class K, bool F16, bool FOLDS>
 __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const TileOperand& A, const TileOperand& B, const int kt0,
                                               const int KT, const int tail, const int rot, f32x16 (&acc)[K::NC][K::NB]) {
   constexpr int NC = K::NC, NB = K::NB, AL = K::AL, BL = K::BL, SA = K::SA, SB = K::SB;
@@ -128,6 +131,22 @@ __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const Ti
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  f32x16 whole[NC][NB];
+  auto fold = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        whole[c][i] += acc[c][i];
+        acc[c][i] = f32x16{};
+      }
+  };
+  if constexpr (FOLDS) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) whole[c][i] = f32x16{};
+  }
   if (KT > 0) {
     // Window t of the loads ends at the barrier of tile t; it brings B of tile t + 2 and A of tile t + SA - 1, A first (a
     // stage is free once the barrier of the tile that it held is passed).  At the barrier of tile t both parts of tile
@@ -169,6 +188,12 @@ __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const Ti
       hard_fence();
     };
     int t = 0;
+    if constexpr (FOLDS) {
+#pragma unroll 1
+      for (; t + K::kChain <= KT - 3; fold())
+#pragma unroll 1
+        for (const int end = t + K::kChain; t < end; ++t) tile(FalseT{}, true, true);
+    }
 #pragma unroll 1
     for (; t < KT - 3; ++t) tile(FalseT{}, true, true);
 #pragma unroll 1
@@ -200,6 +225,12 @@ __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const Ti
       fetch(0, 0, 0, kk);
       mma(0, IntT<4>{}, FalseT{});
     }
+  }
+  if constexpr (FOLDS) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[c][i] += whole[c][i];
   }
 }
 

@@ -238,12 +238,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
   // Products of a group and column tile go to one set of accumulators while those of the one before are scaled and added up in
   // the other, between the MFMAs: the wavefronts run in step, so what one does not overlap by itself is hardly overlapped at all.
   constexpr int SETS = NC * PER > 1 ? 2 : 1;
-  auto compute = [&](const Operands& x, int stage, auto&& midway) __attribute__((always_inline)) {
-    u32x4 later[2][NB];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < NB; ++i) later[j][i] = read_h(stage, j + 2, i);
+  auto compute = [&](const Operands& x, const u32x4 (&later)[2][NB], auto&& midway) __attribute__((always_inline)) {
     f32x16 acc[SETS][NB];
     float scale = 0.f;
     static_for<NC * PER>([&](auto pp) __attribute__((always_inline)) {
@@ -322,6 +317,12 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     __builtin_amdgcn_s_barrier();
     hard_fence();
     const int then = next_of(now), one = stage + 1 == S ? 0 : stage + 1, two = one + 1 == S ? 0 : one + 1, last = stage == 0 ? S - 1 : stage - 1;
+    u32x4 later[2][NB];                                  // this step's rows of the second half, ahead of the next one's in LDS's queue
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) later[j][i] = read_h(stage, j + 2, i);
+    __builtin_amdgcn_sched_barrier(0);
     if (t + S - 1 < T) {
       load_h(h_ahead, last);
       h_ahead = next_of(h_ahead);
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
     }
     if (then == 0) group_at(kb0);
     fetch(1 - ODD, one, keep(then), x[1 - ODD]);         // (behind the last step: something that nobody uses)
-    compute(x[ODD], stage, [&]() __attribute__((always_inline)) {
+    compute(x[ODD], later, [&]() __attribute__((always_inline)) {
       if (t + 2 >= T) return;
       if (t + S < T) wait_early_loads();
       else wait_loads<0>();
@@ -501,34 +502,46 @@ hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
 }
 static_assert(QuantCfg<2, 1, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4 && QuantCfg<1, 2, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4,
               "the scales of one column tile always fit");
-// In how many parts k is dealt over the wavefronts of a workgroup: as few as leave enough workgroups, and as let the scales
-// of its columns fit.
-template <int C, int RB, int HRB>
-hipError_t launch_parts(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
-  const int64_t tiles = up(a.n, kTileCols) / kTileCols, row_tiles = (a.B * a.L + RB * 32 - 1) / (RB * 32);
-  const int64_t work = tiles * row_tiles;
-  using Wide = QuantCfg<C, RB, HRB, 2, 8, 2, 160>;
-  using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
-  using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
-  using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
-  if (work >= 1536 && whole_blocks(q) && scales_fit<Wide>(q)) return launch<Wide>(a, q, s);
-  if (work >= 1536 && scales_fit<One>(q)) return launch<One>(a, q, s);
-  if (work >= 768 && scales_fit<Two>(q)) return launch<Two>(a, q, s);
-  if constexpr (HRB == 8) {
-    using Small = QuantCfg<C, RB, HRB, 1, 4, 4, 80>;
-    if (scales_fit<Small>(q)) return launch<Small>(a, q, s);
-  }
-  return launch<Four>(a, q, s);
+// Which workgroups serve a call: those whose rounds (of as many as run at once) cost least, among those that the scales of
+// their columns fit into.  A round's cost is the time of one on d = 4096, it hardly depends on how full the round is:
+// 32 rows with guidance x 8192 ids take 29 us with four wavefronts sharing a tile (Four), 34 with two (Two), 48 with two tiles per
+// wavefront and k in two parts (Wide); x 16384 55 : 35 : 48, x 32768 105 : 37 : 49, x 65536 209 : 69 : 52; without guidance over
+// 1280 x 8192 9.2 : 11.7 : 15.5, x 65536 61 : 24 : 18; one row x 8192 12.4 : 22.6 : 30, x 65536 87 : 48 : 35.  Tiles of 256 rows (Tall) keep up with
+// Wide nowhere (480 rows with guidance x 8192 115 : 98), but serve groups whose scales do not fit it (groups of 64 with zero
+// points, there 114 : 137 of Two).  One serves long rows of groups that end inside blocks.
+template <class K>
+int64_t cost_of(const LmHeadArgs& a, const QuantizedArgs& q, int resident, int round) {
+  if (!scales_fit<K>(q)) return INT64_MAX;
+  const int64_t tiles = up(a.n, kTileCols) / kTileCols, groups = (tiles + K::COLTILES - 1) / K::COLTILES;
+  const int64_t row_tiles = (static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32);
+  return (groups * row_tiles + resident - 1) / resident * round;
 }
-
-// Many rows: 256 of h and 128 columns (64 where groups end inside blocks) per workgroup, a quarter of the rows per wavefront.
-// False: the scales do not fit.
-template <int C, int NC>
-bool try_tiles(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
-  using Tiles = QuantCfg<C, 8 / C, 32, NC, 8, 1, 160, 4>;
-  if (!scales_fit<Tiles>(q)) return false;
-  (void)launch<Tiles>(a, q, s);
-  return true;
+template <int C, int RB, int HRB>
+hipError_t launch_best(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
+  using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
+  using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
+  using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
+  using Wide = QuantCfg<C, RB, HRB, 2, 8, 2, 160>;
+  using Tall = QuantCfg<C, 8 / C, 32, 2, 8, 1, 160, 4>;          // a quarter of 256 rows per wavefront
+  const bool whole = whole_blocks(q);
+  hipError_t (*best)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t) = launch<Four>;
+  int64_t least = cost_of<Four>(a, q, 256, HRB == 8 ? 13 : 29);
+  auto consider = [&](int64_t cost, hipError_t (*f)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t)) {
+    if (cost < least) {
+      least = cost;
+      best = f;
+    }
+  };
+  consider(cost_of<Two>(a, q, 256, HRB == 8 ? 23 : 35), launch<Two>);
+  consider(cost_of<One>(a, q, 256, HRB == 8 ? 40 : 57), launch<One>);
+  if (whole) consider(cost_of<Wide>(a, q, 256, HRB == 8 ? 31 : 51), launch<Wide>);
+  if constexpr (HRB == 8) {
+    using Small = QuantCfg<C, RB, HRB, 1, 4, 4, 80>;             // two of them per CU
+    consider(cost_of<Small>(a, q, 512, 15), launch<Small>);
+  } else {
+    if (whole) consider(cost_of<Tall>(a, q, 256, 115), launch<Tall>);
+  }
+  return best(a, q, s);
 }
 
 }  // namespace
@@ -563,18 +576,9 @@ hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int
   q.scales = static_cast<const char*>(packed) + padded_tiles(a.n) * k_blocks(a.d) * kBlockBytes;
   q.group = group; q.groups = (a.d + group - 1) / group; q.zeros = zeros;
   const int rows = a.B * a.L;
-  if (rows > 128 / a.C) {
-    const bool done = a.C == 2 ? (whole_blocks(q) ? try_tiles<2, 2>(a, q, s) : try_tiles<2, 1>(a, q, s))
-                               : (whole_blocks(q) ? try_tiles<1, 2>(a, q, s) : try_tiles<1, 1>(a, q, s));
-    if (done) return hipGetLastError();
-  }
-  if (a.C == 2) {
-    if (rows <= 8) return launch_parts<2, 1, 8>(a, q, s);
-    return launch_parts<2, 1, 32>(a, q, s);
-  }
-  if (rows <= 8) return launch_parts<1, 1, 8>(a, q, s);
-  if (rows <= 32) return launch_parts<1, 1, 32>(a, q, s);
-  return launch_parts<1, 2, 32>(a, q, s);
+  if (a.C == 2) return rows <= 8 ? launch_best<2, 1, 8>(a, q, s) : launch_best<2, 1, 32>(a, q, s);
+  if (rows <= 8) return launch_best<1, 1, 8>(a, q, s);
+  return rows <= 32 ? launch_best<1, 1, 32>(a, q, s) : launch_best<1, 2, 32>(a, q, s);
 }
 
 }  // namespace scd

@@ -190,6 +190,26 @@ def test_peaked_and_flat_rows():
     assert abs(got["loss"][0].item() - math.log(n)) < 1e-5
 
 
+def test_small_losses_keep_their_digits():
+    """Rows that are all but sure of their target: the loss is log(1 + r), r = sum of exp(z - z_t), and errs by r times the
+    errors of logits' differences (2 E each) and a few roundings of 1 + r, not by roundings of the logits' size (300 here)."""
+    rows, n, d = 40, 500, 64
+    g = torch.Generator(device="cuda").manual_seed(9)
+    W = torch.randn(n, d, device="cuda", generator=g).to(torch.bfloat16)
+    t = torch.randint(0, n, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    h = (W[t.long()].float() * torch.linspace(0.2, 6.0, rows, device="cuda")[:, None]).to(torch.bfloat16)
+    got = _run(_ctx(n, d), h, W, t, None, torch.bfloat16)["loss"].double()
+    z = h.double() @ W.double().t()
+    E = (h.double().abs() @ W.double().abs().t() * (4 * math.sqrt(d) * U) + 2 * U * z.abs()).amax(1)
+    zt = torch.gather(z, 1, t.long()[:, None])
+    r = torch.exp(z - zt).sum(1) - 1
+    want = torch.log1p(r)
+    # the sum holds 1 and r in 32 bits, tree by tree: 16 roundings of it; its logarithm one more
+    bound = 2 * E * r / (1 + r) + 16 * U * (1 + z.abs().amax(1) * r / (1 + r)) + 2 * U * want
+    assert ((got - want).abs() <= bound).all(), ((got - want).abs() / bound).max().item()
+    assert (want < 1e-4).sum() > 5 and (got >= 0).all()
+
+
 def test_rows_that_are_not_finite_stay_by_themselves():
     rows, n, d = 50, 300, 64
     h, W, t, w = _inputs(rows, n, d, n, 0, seed=6, out=0.0)
