@@ -16,7 +16,7 @@
 // as two terms (22 bits), at the price of a fifth product.  Statistics and sums are fp32.
 //   Bound by the matrix pipes: 4096 rows x 65536 ids over 4096 take 7.8 ms, the four products at 1.15 to 1.25 PFLOP/s (6.2 ms at the 1.42
 // of a large library product), turning W 220 us, its largest element 108, dh's sums over the pieces about 100; the forward pass of 2304 rows
-// 1.06 ms (1.17 PFLOP/s).  Few rows are bound by W: 77 x 16384 over 1280 16.4 us, 42 MB.
+// 1.06 ms (1.17 PFLOP/s).  Few rows are bound by W: 77 x 16384 over 1280 16.6 us, 42 MB.
 #include "gemm_tile.h"
 #include "scd_device.h"
 #include "scd_kernels.h"

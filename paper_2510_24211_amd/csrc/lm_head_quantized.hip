@@ -19,7 +19,7 @@
 // rows and take 1/WK of k each (their sums are added up at the end in a fixed order), WR share tiles and take a part of the rows
 // each.  Weights and h rows go from memory straight into LDS, S stages deep.  The scales of the workgroup's columns are fetched whole at
 // the start.
-//   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096 take 56 us, of which the loads alone would take 25 to 30 (142 MB); a
+//   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096 take 54 us, of which the loads alone would take 25 to 30 (142 MB); a
 // wavefront issues about 220 vector instructions per step of two tiles (64 convert codes, 64 scale, 30 add rows up) beside 20 MFMAs, and the
 // matrix pipes are busy a quarter of the time.  With the offsets taken off by a product with ones it took 75, as C operands from LDS 63.
 #include "lm_head_rows.h"
