@@ -152,6 +152,14 @@ def _ptr(t, dtypes, numel, what):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _int32(value, what):
+    """`value` for an int32 argument: ctypes cuts off what does not fit."""
+    value = int(value)
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{what}: {value} does not fit 32 bits")
+    return value
+
+
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
 GRAD_BF16, GRAD_F32 = 0, 1
 _GRAD = {torch.bfloat16: GRAD_BF16, torch.float32: GRAD_F32}
@@ -297,28 +305,29 @@ class Scd:
 
     # -- 4-bit weights ----------------------------------------------------------
     def quantize(self, W, group, codes, scales, zeros=None):
-        c = self.cfg
+        c, group = self.cfg, _int32(group, "group")
         G = -(-c.d // group) if group > 0 else 0
         self._check(self.lib.scd_quantize(
-            self.ctx, _ptr(W, _BF16, c.V * c.d, "W"), int(group), _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"),
+            self.ctx, _ptr(W, _BF16, c.V * c.d, "W"), group, _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"),
             _ptr(scales, _BF16, c.V * G, "scales"), _ptr(zeros, (torch.uint8,), c.V * G, "zeros")), "scd_quantize")
 
     def pack_quantized(self, codes, scales, zeros, group):
         """The weights in the layout that lm_head_quantized and step_quantized read, in memory of their own."""
-        c = self.cfg
-        need = self.lib.scd_quantized_bytes(ctypes.byref(c), int(group), int(zeros is not None))
+        c, group = self.cfg, _int32(group, "group")
+        need = self.lib.scd_quantized_bytes(ctypes.byref(c), group, int(zeros is not None))
         G = -(-c.d // group) if need else 0
-        packed = QuantizedWeights(self._workspace(need, "scd_quantized_bytes"), int(group), zeros is not None)
+        packed = QuantizedWeights(self._workspace(need, "scd_quantized_bytes"), group, zeros is not None)
         self._check(self.lib.scd_pack_quantized(
             self.ctx, _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"), _ptr(scales, _BF16, c.V * G, "scales"),
-            _ptr(zeros, (torch.uint8,), c.V * G, "zeros"), int(group), ctypes.c_void_p(packed.data.data_ptr())), "scd_pack_quantized")
+            _ptr(zeros, (torch.uint8,), c.V * G, "zeros"), group, ctypes.c_void_p(packed.data.data_ptr())), "scd_pack_quantized")
         return packed
 
     def _quantized(self, W):
-        need = self.lib.scd_quantized_bytes(ctypes.byref(self.cfg), W.group, int(W.zeros))
+        group = _int32(W.group, "group")
+        need = self.lib.scd_quantized_bytes(ctypes.byref(self.cfg), group, int(W.zeros))
         if need == 0:
             raise ScdError(SCD_EINVAL, "scd_quantized_bytes")
-        return ctypes.byref(ScdQuantized(_ptr(W.data, (torch.uint8,), need, "quantized weights"), W.group, int(W.zeros)))
+        return ctypes.byref(ScdQuantized(_ptr(W.data, (torch.uint8,), need, "quantized weights"), group, int(W.zeros)))
 
     def lm_head_quantized(self, h, W, z):
         c = self.cfg
@@ -340,7 +349,7 @@ class Scd:
 
     def embed(self, ids, W, scale, x):
         """x[r] = scale * W[ids[r]] for every id of `ids`; zeros for ids outside [0, V)."""
-        c, rows = self.cfg, ids.numel()
+        c, rows = self.cfg, _int32(ids.numel(), "ids")
         self._check(self.lib.scd_embed(
             self.ctx, _ptr(ids, (torch.int32,), rows, "ids"), rows, _ptr(W, _BF16, c.V * c.d, "W"), float(scale),
             _ptr(x, _BF16, rows * c.d, "x")), "scd_embed")
@@ -352,24 +361,24 @@ class Scd:
             _ptr(x, _BF16, c.B * self.C * c.L * c.d, "x")), "scd_embed_window")
 
     def embed_backward_workspace(self, rows):
-        return self._workspace(self.lib.scd_embed_backward_workspace_bytes(ctypes.byref(self.cfg), rows),
+        return self._workspace(self.lib.scd_embed_backward_workspace_bytes(ctypes.byref(self.cfg), _int32(rows, "rows")),
                                "scd_embed_backward_workspace_bytes")
 
     def embed_backward(self, ids, dx, scale, dW, workspace, accumulate=False):
         """dW (bf16 or fp32) = or += scale * the sums of dx's rows by id."""
-        c, rows = self.cfg, ids.numel()
+        c, rows = self.cfg, _int32(ids.numel(), "ids")
         self._check(self.lib.scd_embed_backward(
             self.ctx, _ptr(ids, (torch.int32,), rows, "ids"), rows, _ptr(dx, _BF16, rows * c.d, "dx"), float(scale),
             _ptr(dW, tuple(_GRAD), c.V * c.d, "dW"), _grad_type(dW.dtype), int(accumulate),
             _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()), "scd_embed_backward")
 
     def cross_entropy_workspace(self, rows):
-        return self._workspace(self.lib.scd_cross_entropy_workspace_bytes(ctypes.byref(self.cfg), rows),
+        return self._workspace(self.lib.scd_cross_entropy_workspace_bytes(ctypes.byref(self.cfg), _int32(rows, "rows")),
                                "scd_cross_entropy_workspace_bytes")
 
     def cross_entropy(self, h, W, targets, loss, lse, workspace):
         """One loss and log normaliser per target; a negative target leaves its row out."""
-        c, rows = self.cfg, targets.numel()
+        c, rows = self.cfg, _int32(targets.numel(), "targets")
         self._check(self.lib.scd_cross_entropy(
             self.ctx, _ptr(h, _BF16, rows * c.d, "h"), _ptr(W, _BF16, c.V * c.d, "W"),
             _ptr(targets, (torch.int32,), rows, "targets"), rows, _ptr(loss, (torch.float32,), rows, "loss"),
@@ -378,11 +387,11 @@ class Scd:
 
     def cross_entropy_backward_workspace(self, rows, grad_dtype=torch.bfloat16):
         return self._workspace(self.lib.scd_cross_entropy_backward_workspace_bytes(
-            ctypes.byref(self.cfg), rows, _grad_type(grad_dtype)), "scd_cross_entropy_backward_workspace_bytes")
+            ctypes.byref(self.cfg), _int32(rows, "rows"), _grad_type(grad_dtype)), "scd_cross_entropy_backward_workspace_bytes")
 
     def cross_entropy_backward(self, h, W, targets, lse, weight, dh, dW, workspace, accumulate=False):
         """Gradients of sum(weight * loss) (weight None: 1); dh or dW may be None."""
-        c, rows = self.cfg, targets.numel()
+        c, rows = self.cfg, _int32(targets.numel(), "targets")
         self._check(self.lib.scd_cross_entropy_backward(
             self.ctx, _ptr(h, _BF16, rows * c.d, "h"), _ptr(W, _BF16, c.V * c.d, "W"),
             _ptr(targets, (torch.int32,), rows, "targets"), rows, _ptr(lse, (torch.float32,), rows, "lse"),
