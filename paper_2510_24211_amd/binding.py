@@ -172,10 +172,12 @@ def _grad_type(dtype):
 
 
 class QuantizedWeights:
-    """4-bit weights as pack_quantized lays them out for one configuration."""
+    """4-bit weights as pack_quantized lays them out for one configuration's allowed ids and width; cfg = None: the
+    caller answers for that."""
 
-    def __init__(self, data, group, zeros):
+    def __init__(self, data, group, zeros, cfg=None):
         self.data, self.group, self.zeros = data, group, zeros
+        self.rows = None if cfg is None else (cfg.v_lo, cfg.v_hi, cfg.d)
 
 
 class Scd:
@@ -316,14 +318,16 @@ class Scd:
         c, group = self.cfg, _int32(group, "group")
         need = self.lib.scd_quantized_bytes(ctypes.byref(c), group, int(zeros is not None))
         G = -(-c.d // group) if need else 0
-        packed = QuantizedWeights(self._workspace(need, "scd_quantized_bytes"), group, zeros is not None)
+        packed = QuantizedWeights(self._workspace(need, "scd_quantized_bytes"), group, zeros is not None, c)
         self._check(self.lib.scd_pack_quantized(
             self.ctx, _ptr(codes, (torch.uint8,), c.V * c.d // 2, "codes"), _ptr(scales, _BF16, c.V * G, "scales"),
             _ptr(zeros, (torch.uint8,), c.V * G, "zeros"), group, ctypes.c_void_p(packed.data.data_ptr())), "scd_pack_quantized")
         return packed
 
     def _quantized(self, W):
-        group = _int32(W.group, "group")
+        group, rows = _int32(W.group, "group"), (self.cfg.v_lo, self.cfg.v_hi, self.cfg.d)
+        if W.rows not in (None, rows):
+            raise ValueError(f"quantized weights: laid out for (v_lo, v_hi, d) = {W.rows}, not for {rows}")
         need = self.lib.scd_quantized_bytes(ctypes.byref(self.cfg), group, int(W.zeros))
         if need == 0:
             raise ScdError(SCD_EINVAL, "scd_quantized_bytes")

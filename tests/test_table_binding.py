@@ -59,3 +59,17 @@ def test_rows_that_32_bits_do_not_hold_are_refused(rows):
     for call in calls:
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("other", [dict(V=100, v_lo=10, v_hi=42, d=64), dict(V=100, v_lo=0, v_hi=32, d=40)])
+def test_weights_laid_out_for_other_ids_are_refused(other):
+    """Rows 10 .. 41 of a table take the bytes of rows 0 .. 31, and so do rows of 40 weights those of 64."""
+    s = _scd(V=100, v_lo=0, v_hi=32)
+    c = B.make_config(B=1, L=1, N=1, **other)
+    need = s.lib.scd_quantized_bytes(ctypes.byref(c), 64, 0)
+    assert need == s.lib.scd_quantized_bytes(ctypes.byref(s.cfg), 64, 0)
+    h, z, st = _gpu(torch.bfloat16, 64), _gpu(torch.float32, 32), _gpu(torch.uint8, B.state_bytes(s.cfg))
+    W = B.QuantizedWeights(_gpu(torch.uint8, need), 64, False, c)
+    for call in (lambda: s.lm_head_quantized(h, W, z), lambda: s.step_quantized(h, W, st)):
+        with pytest.raises(ValueError, match="laid out for"):
+            call()
