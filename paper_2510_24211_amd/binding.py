@@ -192,8 +192,8 @@ class Scd:
         need = self.lib.scd_workspace_bytes(ctypes.byref(cfg))
         if need == 0:
             raise ScdError(SCD_EINVAL, "scd_workspace_bytes")
-        self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self.workspace = self._empty(need)
         ctx = ctypes.c_void_p()
         rc = self.lib.scd_create(ctypes.byref(ctx), ctypes.byref(cfg),
                                  ctypes.c_void_p(self.workspace.data_ptr()), need,
@@ -215,10 +215,14 @@ class Scd:
         if rc != SCD_OK:
             raise ScdError(rc, what)
 
+    def _empty(self, nbytes):
+        """Memory of the context's stream: what another stream has freed may be in use there still."""
+        with torch.cuda.stream(self.stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
     # -- state ------------------------------------------------------------
     def alloc_state(self):
-        nbytes = self.lib.scd_state_bytes(ctypes.byref(self.cfg))
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return self._empty(self.lib.scd_state_bytes(ctypes.byref(self.cfg)))
 
     def state_field(self, state, field):
         """A tensor view of one field of the state buffer."""
@@ -349,7 +353,7 @@ class Scd:
     def _workspace(self, need, what):
         if need == 0:
             raise ScdError(SCD_EINVAL, what)
-        return torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._empty(need)
 
     def embed(self, ids, W, scale, x):
         """x[r] = scale * W[ids[r]] for every id of `ids`; zeros for ids outside [0, V)."""
