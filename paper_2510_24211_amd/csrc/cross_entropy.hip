@@ -12,8 +12,10 @@
 // short, so every operand is brought under 2^15 by a power of two: W and the rows of h by the exponent of their largest finite
 // element (range_kernel reads them once), dz, which lies in [-1, 1] without the rows' weights, by 2^14, and with
 // the weights for dW by the exponent of the largest.  The elements of W and h, of 8 bits, stay exact down to 2^-31 of the
-// largest; dz has its 11 bits down to 2^-28, and an absolute error of 2^-39 below.  Where dW is kept in 32 bits dz enters its product
-// as two terms (22 bits), at the price of a fifth product.  Statistics and sums are fp32.
+// largest; dz has its 11 bits down to 2^-28 of the largest weight, and an absolute error of 2^-39 of it below.  Where dW is kept in 32 bits
+// dz enters its product as two terms, at the price of a fifth product: what the first one leaves, times 2^11, has sums of its own, which
+// are brought down again before the first terms' are added to them.  So dz errs by 2^-22 of itself or 2^-50 of the largest
+// weight, whichever is more.  Statistics and sums are fp32.
 //   Bound by the matrix pipes: 4096 rows x 65536 ids over 4096 take 7.8 ms, the four products at 1.15 to 1.25 PFLOP/s (6.2 ms at the 1.42
 // of a large library product), turning W 220 us, its largest element 108, dh's sums over the pieces about 100; the forward pass of 2304 rows
 // 1.06 ms (1.17 PFLOP/s).  Few rows are bound by W: 77 x 16384 over 1280 16.6 us, 42 MB.
@@ -39,20 +41,21 @@ __device__ __forceinline__ float half_fold(float v, F&& f) {
   return f(v, __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x401F)));     // lane ^ 16
 }
 
-enum GemmUse { kLoss, kGradient, kRows, kTable };
+enum GemmUse { kLoss, kGradient, kRows, kTable, kTableTwoTerms };
 
 // floor(log2) of the largest finite element of the allowed rows of W, of the rows of h and of the weights that count
 struct Exponents {
   int W, h, weight;
 };
 constexpr int kTop = 14;     // operands of the gradient's products lie below 2^(kTop + 1)
+constexpr int kRest = 11;    // the second terms of dz are stored times 2^kRest: what rounding to 11 bits leaves stays below the same bound
 
 struct GemmArgs {
   const uint16_t* A;
   const uint16_t* B;
   int64_t lda, ldb;          // elements from row to row
   int M, N;                  // rows of A, of B
-  int KT, tail, wrapB;       // whole k-tiles, elements of the ragged one; k-tiles after which B's columns begin again
+  int KT, tail;              // whole k-tiles, elements of the ragged one
   int MT, NT, KS;            // tiles, parts of k
   // kLoss, kGradient
   const int32_t* targets;
@@ -66,12 +69,12 @@ struct GemmArgs {
   uint16_t* dzT;             // fp16 [N][ldT], with them: first terms, then (two_terms) the second ones `lo` columns on
   int64_t ldz, ldT;
   int lo;
-  bool two_terms;
-  // kRows: sums [KS][M][N] in fp32, over the pieces of the vocabulary so far; kRows, kTable: result [M][N]
+  bool two_terms;            // to be written (kGradient); kTableTwoTerms takes both, on the same columns of B
+  // kRows: sums [KS][M][N] in fp32, over the pieces of the vocabulary so far; it and the tables: result [M][N]
   float* sums;
   bool first, last;
-  void* out;
-  bool f32, accumulate;
+  void* out;                 // bf16, kTableTwoTerms: fp32
+  bool accumulate;
   const Exponents* exps;
 };
 
@@ -130,14 +133,31 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int i = 0; i < NB; ++i) acc[c][i] = f32x16{};
-  const TileOperand A{reinterpret_cast<uint64_t>(a.A + row0 * a.lda), rows, static_cast<uint32_t>(a.lda * 2), 0x7FFFFFFF};
-  const TileOperand B{reinterpret_cast<uint64_t>(a.B + col0 * a.ldb), cols, static_cast<uint32_t>(a.ldb * 2), a.wrapB};
+  TileOperand A{reinterpret_cast<uint64_t>(a.A + row0 * a.lda), rows, static_cast<uint32_t>(a.lda * 2)};
+  const TileOperand B{reinterpret_cast<uint64_t>(a.B + col0 * a.ldb), cols, static_cast<uint32_t>(a.ldb * 2)};
   // the workgroups of an XCD meet in its L2, the XCDs start at different columns
   const int rot = KT > 0 ? static_cast<int>(static_cast<int64_t>(blockIdx.x % 8) * KT / 8) : 0;
   // 2 rows x 2680 ids over 1688: the loss errs by 1.6e-6 rms in one chain, by 5.6e-7 folded, with no more time
   constexpr bool FOLDS = (USE == kLoss || USE == kGradient) && HR * BN <= 128 * 128;
-  multiply_tile<K, USE == kRows || USE == kTable, FOLDS>(lds, A, B, kt0, KT, a.tail, rot, acc);
-  __syncthreads();
+  constexpr bool F16 = USE != kLoss && USE != kGradient;
+  if constexpr (USE == kTableTwoTerms) {
+    const uint64_t first = A.base;
+    A.base += static_cast<uint64_t>(a.lo) * 2u;
+#pragma unroll 1
+    for (int term = 1; term >= 0; --term) {
+      multiply_tile<K, F16, FOLDS>(lds, A, B, kt0, KT, a.tail, rot, acc);
+      __syncthreads();
+      A.base = first;
+      const float down = term == 1 ? 1.f / (1 << kRest) : 1.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[c][i] *= down;
+    }
+  } else {
+    multiply_tile<K, F16, FOLDS>(lds, A, B, kt0, KT, a.tail, rot, acc);
+    __syncthreads();
+  }
 
   if constexpr (USE == kLoss || USE == kGradient) {
     int* const target = reinterpret_cast<int*>(lds);
@@ -240,7 +260,7 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   b[e] = f16_bits(acc[c][i][4 * g + e]);
-                  acc[c][i][4 * g + e] -= f16_value(b[e]);       // the rest, for the second term
+                  acc[c][i][4 * g + e] = (acc[c][i][4 * g + e] - f16_value(b[e])) * (1 << kRest);       // exact
                 }
                 *reinterpret_cast<uint2*>(tile + (c0 + c * 32) * (HR + 8) + wr * K::RW + i * 32 + g * 8 + lg * 4) =
                     make_uint2(b[0] | static_cast<uint32_t>(b[1]) << 16, b[2] | static_cast<uint32_t>(b[3]) << 16);
@@ -289,7 +309,8 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
 #pragma unroll
           for (int c = 0; c < NC; ++c) acc[c][i][j] = __builtin_ldexpf(acc[c][i][j] * a.inv_tau, e);
     }
-    if (a.f32 || a.accumulate) {
+    constexpr bool F32 = USE == kTableTwoTerms;
+    if (F32 || a.accumulate) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -300,7 +321,7 @@ __global__ __launch_bounds__(512) void gemm_kernel(const GemmArgs a) {
             if (r >= rows || c0 + c * 32 >= cols) continue;
             const int64_t to = static_cast<int64_t>(row0 + r) * a.N + col0 + c0 + c * 32;
             float v = acc[c][i][j];
-            if (a.f32) {
+            if constexpr (F32) {
               float* const p = static_cast<float*>(a.out) + to;
               if (a.accumulate) v += *p;
               *p = v;
@@ -578,7 +599,7 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& c, hipStream_t s) {
   if (c.rows == 0) return hipSuccess;
   GemmArgs a{};
   a.A = c.h; a.B = c.W; a.lda = a.ldb = c.d;
-  a.M = c.rows; a.N = c.n; a.KT = c.d / 64; a.tail = c.d % 64; a.wrapB = 0x7FFFFFFF; a.KS = 1;
+  a.M = c.rows; a.N = c.n; a.KT = c.d / 64; a.tail = c.d % 64; a.KS = 1;
   a.targets = c.targets;
   a.inv_tau = 1.f / c.tau; a.scale2 = kLog2e / c.tau;
   a.zt = static_cast<float*>(c.ws);
@@ -629,7 +650,7 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
     if (c.rows > 0) {
       GemmArgs a{};
       a.A = c.h; a.B = W; a.lda = a.ldb = c.d;
-      a.M = c.rows; a.N = v; a.KT = c.d / 64; a.tail = c.d % 64; a.wrapB = 0x7FFFFFFF; a.KS = 1;
+      a.M = c.rows; a.N = v; a.KT = c.d / 64; a.tail = c.d % 64; a.KS = 1;
       a.targets = c.targets; a.col0 = v0;
       a.inv_tau = 1.f / c.tau; a.scale2 = kLog2e / c.tau;
       a.lse = c.lse; a.weight = c.weight; a.exps = exps;
@@ -641,7 +662,7 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
       if ((e = launch_turn<false>(W, c.d, v, c.d, WT, vpad, static_cast<int>(vpad), nullptr, nullptr, 0, exps, s)) != hipSuccess) return e;
       GemmArgs a{};
       a.A = dz; a.B = WT; a.lda = a.ldb = vpad;
-      a.M = c.rows; a.N = c.d; a.KT = static_cast<int>(vpad / 64); a.wrapB = 0x7FFFFFFF; a.KS = p.parts;
+      a.M = c.rows; a.N = c.d; a.KT = static_cast<int>(vpad / 64); a.KS = p.parts;
       a.sums = sums; a.first = v0 == 0; a.last = p.parts == 1 && v0 + v == c.n;
       a.out = c.dh;
       a.targets = c.targets; a.weight = c.weight; a.inv_tau = 1.f / c.tau; a.exps = exps;
@@ -650,13 +671,13 @@ hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& c, hipStream_t 
     if (c.dW) {
       GemmArgs a{};
       a.A = dzT; a.B = hT; a.lda = p.mpad * terms; a.ldb = p.mpad;
-      a.M = v; a.N = c.d; a.KT = static_cast<int>(p.mpad / 64) * terms; a.wrapB = static_cast<int>(p.mpad / 64); a.KS = 1;
-      if (a.wrapB == 0) a.wrapB = 0x7FFFFFFF;
+      a.M = v; a.N = c.d; a.KT = static_cast<int>(p.mpad / 64); a.KS = 1;
+      a.lo = static_cast<int>(p.mpad);
       a.out = c.f32 ? static_cast<void*>(static_cast<float*>(c.dW) + static_cast<int64_t>(v0) * c.d)
                     : static_cast<void*>(static_cast<uint16_t*>(c.dW) + static_cast<int64_t>(v0) * c.d);
-      a.f32 = c.f32; a.accumulate = c.accumulate;
+      a.accumulate = c.accumulate;
       a.inv_tau = 1.f / c.tau; a.exps = exps;
-      if ((e = launch_gemm<kTable>(a, s)) != hipSuccess) return e;
+      if ((e = c.f32 ? launch_gemm<kTableTwoTerms>(a, s) : launch_gemm<kTable>(a, s)) != hipSuccess) return e;
     }
   }
   if (c.dh && c.rows > 0 && p.parts > 1) {

@@ -25,12 +25,11 @@ struct GemmTile {
 };
 
 // One operand as a workgroup reads it: its first row, `rows` of them exist (past them the last one is read, and what
-// comes of it is not to be stored), `bytes` from row to row.  After `wrap` k-tiles its columns begin again.
+// comes of it is not to be stored), `bytes` from row to row.
 struct TileOperand {
   uint64_t base;
   int rows;
   uint32_t bytes;
-  int wrap;
 };
 
 // acc += the k-tiles kt0 .. kt0 + KT - 1, walked cyclically from the `rot`-th of them, and `tail` (< 64, a multiple of 8)
@@ -74,9 +73,7 @@ __device__ __forceinline__ void multiply_tile(unsigned char* const lds, const Ti
     uint32_t lds;         // the stage it goes to
     int k, n;             // its index; tiles issued before it
   };
-  auto column = [](const TileOperand& o, int k) {
-    return o.base + static_cast<uint64_t>(static_cast<uint32_t>(k >= o.wrap ? k - o.wrap : k)) * 128u;
-  };
+  auto column = [](const TileOperand& o, int k) { return o.base + static_cast<uint64_t>(static_cast<uint32_t>(k)) * 128u; };
   Walk aw{column(A, kt0 + rot), ldsA, kt0 + rot, 0}, bw{column(B, kt0 + rot), ldsB, kt0 + rot, 0};
   auto advance = [&](Walk& w, const TileOperand& o, uint32_t first, uint32_t bytes, int stages) {
     w.k = w.k + 1 == kt0 + KT ? kt0 : w.k + 1;
