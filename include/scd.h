@@ -350,7 +350,11 @@ int scd_cross_entropy(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, co
 /* Its gradient.  d_lse from scd_cross_entropy on the same arguments; d_weight fp32 [rows], the gradient of the result with
  * respect to each row's loss, NULL = 1 (1 / rows for a mean).  The logits are made again, a piece of the vocabulary at a
  * time.  d_dh bf16 [rows, d] and d_dW [V, d] of type grad_type, of which the allowed rows alone are written, or added to
- * with accumulate = 1 (in 32 bits, rounded once); either may be NULL (not wanted).  The same call gives the same bits. */
+ * with accumulate = 1 (in 32 bits, rounded once); either may be NULL (not wanted).  The same call gives the same bits.
+ *   The gradient's products add up in fp32, on operands of 16 bits: the gradients of the logits have 11 bits, down to 2^-28 (of the largest
+ * weight for d_dW; steps of 2^-38 below, so that what is smaller than 2^-39 counts as 0).  For an fp32 d_dW alone they have 22 bits and end
+ * at 2^-50.  W and the rows of h stand under one power of two each: elements below 2^-31 of the largest finite one (of all
+ * allowed rows of W, or of all rows of h that are not left out) lose bits, and those below 2^-39 of it count as 0. */
 size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type);
 int scd_cross_entropy_backward(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
                                const float* d_lse, const float* d_weight, uint16_t* d_dh, void* d_dW, int32_t grad_type,
