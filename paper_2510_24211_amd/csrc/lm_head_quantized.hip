@@ -414,7 +414,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restric
       lo = fminf(lo, __shfl_xor(lo, o, 64));
       hi = fmaxf(hi, __shfl_xor(hi, o, 64));
     }
-    const __bf16 sb = static_cast<__bf16>(zeros ? __fdiv_rn(hi - lo, 15.f) : fmaxf(__fdiv_rn(hi, 7.f), __fdiv_rn(-lo, 8.f)));
+    // (halves, exactly: the range of finite weights may not be finite)
+    const __bf16 sb = static_cast<__bf16>(zeros ? __fdiv_rn(0.5f * hi - 0.5f * lo, 7.5f) : fmaxf(__fdiv_rn(hi, 7.f), __fdiv_rn(-lo, 8.f)));
     const float s = static_cast<float>(sb);
     const int zero = zeros && s > 0.f ? static_cast<int>(fminf(rintf(__fdiv_rn(-lo, s)), 15.f)) : 8;
     auto code = [&](float x) {
