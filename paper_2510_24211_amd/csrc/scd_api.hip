@@ -358,8 +358,9 @@ int couple_draft_impl(scd_ctx* c, char* w, bool cands, const float* d_z_cur, con
 
 // What the operators on the vocabulary table check alike.
 constexpr int32_t kCrossEntropyRows = 1 << 20, kEmbedRows = 1 << 25, kEmbedWidth = 1 << 24, kMostIds = 1 << 30;
-inline bool cross_entropy_fits(int32_t rows, int32_t n, int32_t d) {      // tiles that one launch can hold, rows that 32 bits reach
-  return n <= kMostIds && d <= (1 << 21) && static_cast<int64_t>(rows) * n <= static_cast<int64_t>(1) << 38;
+inline bool cross_entropy_fits(int32_t rows, int32_t n, int32_t d, float tau) {      // tiles that one launch can hold, rows that 32 bits reach
+  return n <= kMostIds && d <= (1 << 21) && static_cast<int64_t>(rows) * n <= static_cast<int64_t>(1) << 38 &&
+         std::isfinite(1.4426950408889634f / tau);         // (differences of 0 are multiplied by it)
 }
 inline bool valid_gradient(int32_t grad_type, int32_t accumulate) {
   return (grad_type == SCD_GRAD_BF16 || grad_type == SCD_GRAD_F32) && (accumulate == 0 || accumulate == 1);
@@ -386,7 +387,7 @@ int cross_entropy_args(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, con
                        scd::CrossEntropyArgs* a) {
   if (!d_W || rows < 0 || rows > kCrossEntropyRows || (rows > 0 && (!d_h || !d_targets)) || c->cfg.d <= 0) return SCD_EINVAL;
   if (!aligned(d_h, 16) || !aligned(d_W, 16) || !aligned(d_targets, 4)) return SCD_EINVAL;
-  if (c->C != 1 || !cross_entropy_fits(rows, c->n, c->cfg.d)) return SCD_EUNSUPPORTED;
+  if (c->C != 1 || !cross_entropy_fits(rows, c->n, c->cfg.d, c->cfg.temperature)) return SCD_EUNSUPPORTED;
   a->h = d_h;
   a->W = d_W + static_cast<size_t>(c->cfg.v_lo) * c->cfg.d;
   a->targets = d_targets;
@@ -599,13 +600,13 @@ int scd_embed_backward(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uin
 }
 
 size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows) {
-  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d)) return 0;
+  if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d, cfg->temperature)) return 0;
   return scd::cross_entropy_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d);
 }
 
 size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type) {
   if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !valid_gradient(grad_type, 0) ||
-      !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d))
+      !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d, cfg->temperature))
     return 0;
   return scd::cross_entropy_backward_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d, grad_type == SCD_GRAD_F32);
 }
