@@ -341,8 +341,8 @@ int scd_embed_backward(scd_ctx* ctx, const int32_t* d_ids, int32_t rows, const u
  * top_k, top_p and the decode options do not enter; cfg_lambda must be 0 (SCD_EUNSUPPORTED otherwise).
  *   d_h bf16 [rows, d];  d_targets int32 [rows], OFFSETS into the allowed ids; a negative one leaves the row out (loss 0,
  * no gradient, whatever the row holds), one of n or more is not an allowed id (loss +inf, gradient of the normaliser alone);
- *   d_loss, d_lse fp32 [rows], written.  rows * allowed ids up to 2^38, d up to 2^21, tau such that log2(e) / tau is finite
- * (SCD_EUNSUPPORTED beyond). */
+ *   d_loss, d_lse fp32 [rows], written.  rows * allowed ids up to 2^38, allowed ids up to 2^30, d up to 2^21, tau
+ * such that log2(e) / tau is finite (SCD_EUNSUPPORTED beyond). */
 size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows);
 int scd_cross_entropy(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, const int32_t* d_targets, int32_t rows,
                       float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes);
