@@ -433,27 +433,27 @@ __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restric
   }
 }
 
-// A wavefront per column tile and block of k: 16 bytes per lane.
+// A wavefront per column tile and block of k: 16 bytes per lane.  (Tables of 64 GiB have more of them than a launch has threads for.)
 __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t* __restrict__ codes, int n, int d, int KB, int64_t blocks,
                                                          u32x4* __restrict__ to) {
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (item >= blocks) return;
   const int lane = threadIdx.x & 63;
-  const int64_t v = item / KB * kTileCols + (lane & 31);
-  const int k0 = static_cast<int>(item % KB) * kBlockK + (lane >> 5) * 8;
-  u32x4 out{0u, 0u, 0u, 0u};
+  for (int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); item < blocks; item += static_cast<int64_t>(gridDim.x) * 4) {
+    const int64_t v = item / KB * kTileCols + (lane & 31);
+    const int k0 = static_cast<int>(item % KB) * kBlockK + (lane >> 5) * 8;
+    u32x4 out{0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int k = k0 + j * 16;
-    if (v < n && k < d) {                       // d is a multiple of 8
-      const uint32_t in = *reinterpret_cast<const uint32_t*>(codes + v * (d / 2) + k / 2);      // code t at bits 4 t
-      uint32_t w = 0u;
+    for (int j = 0; j < 4; ++j) {
+      const int k = k0 + j * 16;
+      if (v < n && k < d) {                       // d is a multiple of 8
+        const uint32_t in = *reinterpret_cast<const uint32_t*>(codes + v * (d / 2) + k / 2);      // code t at bits 4 t
+        uint32_t w = 0u;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) w |= (in >> (4 * t) & 15u) << ((t & 1) * 16 + (t >> 1) * 4);
-      out[j] = w;
+        for (int t = 0; t < 8; ++t) w |= (in >> (4 * t) & 15u) << ((t & 1) * 16 + (t >> 1) * 4);
+        out[j] = w;
+      }
     }
+    to[item * 64 + lane] = out;
   }
-  to[item * 64 + lane] = out;
 }
 __global__ __launch_bounds__(256) void pack_scales_kernel(const uint16_t* __restrict__ scales, const uint8_t* __restrict__ zeros, int n, int groups,
                                                           int64_t count, void* __restrict__ to) {
@@ -563,8 +563,8 @@ hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, c
                                  hipStream_t s) {
   const int64_t tiles = padded_tiles(n), blocks = tiles * k_blocks(d);
   const int groups = (d + group - 1) / group;
-  hipLaunchKernelGGL(pack_codes_kernel, dim3(static_cast<uint32_t>((blocks + 3) / 4)), dim3(256), 0, s, codes, n, d, k_blocks(d), blocks,
-                     static_cast<u32x4*>(packed));
+  hipLaunchKernelGGL(pack_codes_kernel, dim3(static_cast<uint32_t>((blocks + 3) / 4 < kMostBlocks ? (blocks + 3) / 4 : kMostBlocks)), dim3(256), 0, s, codes, n, d,
+                     k_blocks(d), blocks, static_cast<u32x4*>(packed));
   const int64_t count = tiles * groups * kTileCols;
   hipLaunchKernelGGL(pack_scales_kernel, dim3(static_cast<uint32_t>((count + 255) / 256 < kMostBlocks ? (count + 255) / 256 : kMostBlocks)), dim3(256), 0, s, scales, zeros, n, groups, count,
                      static_cast<char*>(packed) + blocks * kBlockBytes);

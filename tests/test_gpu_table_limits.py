@@ -39,3 +39,29 @@ def test_cross_entropy_over_2_30_ids(rows):
     # p to 64 u (1 + z) of itself, 2^-11 of dz, 2^-8 of the result; zero columns stay zero
     assert ((dh[:, 0].double() - wanted).abs() <= wanted.abs() * (2.0 ** -8 + 2.0 ** -10)).all()
     assert not dh[:, 1:].any()
+
+
+def test_a_packed_table_of_64_gib():
+    """2^37 codes: those of the first and the last rows are where they belong (logits of whole numbers, exact)."""
+    n, d = 1 << 30, 128
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GiB")
+    s = B.Scd(B.make_config(B=1, L=1, N=1, V=n, d=d))
+    codes = torch.full((n, d // 2), 0x88, dtype=torch.uint8, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for at in (0, n // 2, n - 40):
+        codes[at:at + 40] = torch.randint(0, 256, (40, d // 2), device="cuda", generator=g, dtype=torch.uint8)
+    W = s.pack_quantized(codes, torch.ones(n, 1, dtype=torch.bfloat16, device="cuda"), None, 128)
+    h = torch.randint(-8, 9, (1, 1, 1, d), device="cuda", generator=g).to(torch.bfloat16)
+    z = torch.full((1, 1, n), 7.0, device="cuda")
+    s.lm_head_quantized(h, W, z)
+    q = lambda at: torch.stack([codes[at:at + 40] & 15, codes[at:at + 40] >> 4], 2).reshape(40, d).double() - 8  # noqa: E731
+    for at in (0, n // 2, n - 40):
+        assert torch.equal(z[0, 0, at:at + 40].double(), q(at) @ h[0, 0, 0].double()), at
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    for at in (0, n // 2, n - 40):
+        rest[at:at + 40] = False
+    assert not z[0, 0, rest].any()
+    del codes, W, z, rest
+    torch.cuda.empty_cache()
