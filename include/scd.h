@@ -252,7 +252,7 @@ int scd_verify(scd_ctx* ctx, const uint8_t* d_k, const int32_t* d_y, const int32
 int scd_step(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, void* d_state);
 
 /* Optional instrumentation for benchmarks: while both events are non-NULL,
- * scd_step launches the LM-head kernel with the two events attached to the
+ * scd_step and scd_step_quantized launch the LM-head kernel with the two events attached to the
  * dispatch (hipExtLaunchKernel): ev_start takes the kernel's start time, ev_stop
  * its stop time, on the context's stream; no other packet enters the stream
  * (hipEvent_t passed as void*, owned by the caller).  NULL, NULL turns it off.

@@ -22,10 +22,9 @@
 // live in the same lanes, so the guidance mix needs no data movement; every workgroup walks k cyclically
 // from its own starting tile: rows of W are d*2 bytes apart, and without the rotation all of the chip asks for
 // the same address bits at the same time and camps on a few channels.
+#include "launch_events.h"
 #include "lm_head_rows.h"
 #include "tile_loads.h"
-
-#include <hip/hip_ext.h>
 
 #include <stdio.h>
 
@@ -1216,17 +1215,6 @@ RowMap make_row_map(const LmHeadArgs& a, int BN, int VT, int* tiles_per_xcd) {
   const long rows_per_xcd = (groups + 7) / 8 * G;
   *tiles_per_xcd = static_cast<int>((rows_per_xcd + BN - 1) / BN);
   return m;
-}
-
-// Optional timing of the launch: the runtime attaches the two events to the dispatch itself
-// (start and stop time of the kernel), so no marker packets of their own enter the stream.
-struct LaunchEvents {
-  hipEvent_t start, stop;
-};
-template <class Kern, class... Args>
-void launch_kernel(Kern kernel, dim3 grid, dim3 block, hipStream_t s, const LaunchEvents& ev, Args... args) {
-  if (ev.start && ev.stop) hipExtLaunchKernelGGL(kernel, grid, block, 0, s, ev.start, ev.stop, 0, args...);
-  else hipLaunchKernelGGL(kernel, grid, block, 0, s, args...);
 }
 
 // W is streamed past the caches when its slice cannot stay in the memory-side cache anyway

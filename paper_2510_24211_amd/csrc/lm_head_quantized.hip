@@ -22,6 +22,7 @@
 //   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096 take 54 us, of which the loads alone would take 25 to 30 (142 MB); a
 // wavefront issues about 220 vector instructions per step of two tiles (64 convert codes, 64 scale, 30 add rows up) beside 20 MFMAs, and the
 // matrix pipes are busy a quarter of the time.  With the offsets taken off by a product with ones it took 75, as C operands from LDS 63.
+#include "launch_events.h"
 #include "lm_head_rows.h"
 #include "tile_loads.h"
 
@@ -482,22 +483,22 @@ bool scales_fit(const QuantizedArgs& q) {
   return up(static_cast<int64_t>(K::COLTILES) * q.groups * kTileCols * (q.zeros ? 4 : 2), 1024) <= K::SCALES;
 }
 template <class K, int STEP>
-void launch_step(const LmHeadArgs& a, const QuantizedArgs& q, dim3 grid, int WT, int MT, hipStream_t s) {
-  if (q.zeros) hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, true>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
-  else hipLaunchKernelGGL((lm_head_quantized_kernel<K, STEP, false>), grid, dim3(K::THREADS), 0, s, a, q, WT, MT);
+void launch_step(const LmHeadArgs& a, const QuantizedArgs& q, dim3 grid, int WT, int MT, hipStream_t s, const LaunchEvents& ev) {
+  if (q.zeros) launch_kernel(lm_head_quantized_kernel<K, STEP, true>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
+  else launch_kernel(lm_head_quantized_kernel<K, STEP, false>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
 }
 // Two column tiles per wavefront leave no registers for groups that end inside a block: those have one.
 inline bool whole_blocks(const QuantizedArgs& q) { return q.group % kBlockK == 0; }
 template <class K>
-hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
+hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s, const LaunchEvents& ev) {
   const int64_t tiles = up(a.n, kTileCols) / kTileCols;
   const int WT = static_cast<int>((tiles + K::COLTILES - 1) / K::COLTILES), MT = (a.B * a.L + K::RB * 32 - 1) / (K::RB * 32);
   const dim3 grid((WT + 7) / 8 * 8 * MT);
   if constexpr (K::NC == 2) {
-    launch_step<K, 4>(a, q, grid, WT, MT, s);
+    launch_step<K, 4>(a, q, grid, WT, MT, s, ev);
   } else {
-    if (whole_blocks(q)) launch_step<K, 4>(a, q, grid, WT, MT, s);
-    else launch_step<K, 2>(a, q, grid, WT, MT, s);
+    if (whole_blocks(q)) launch_step<K, 4>(a, q, grid, WT, MT, s, ev);
+    else launch_step<K, 2>(a, q, grid, WT, MT, s, ev);
   }
   return hipGetLastError();
 }
@@ -518,16 +519,16 @@ int64_t cost_of(const LmHeadArgs& a, const QuantizedArgs& q, int resident, int r
   return (groups * row_tiles + resident - 1) / resident * round;
 }
 template <int C, int RB, int HRB>
-hipError_t launch_best(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s) {
+hipError_t launch_best(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s, const LaunchEvents& ev) {
   using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
   using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
   using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
   using Wide = QuantCfg<C, RB, HRB, 2, 8, 2, 160>;
   using Tall = QuantCfg<C, 8 / C, 32, 2, 8, 1, 160, 4>;          // a quarter of 256 rows per wavefront
   const bool whole = whole_blocks(q);
-  hipError_t (*best)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t) = launch<Four>;
+  hipError_t (*best)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t, const LaunchEvents&) = launch<Four>;
   int64_t least = cost_of<Four>(a, q, 256, HRB == 8 ? 13 : 29);
-  auto consider = [&](int64_t cost, hipError_t (*f)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t)) {
+  auto consider = [&](int64_t cost, hipError_t (*f)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t, const LaunchEvents&)) {
     if (cost < least) {
       least = cost;
       best = f;
@@ -542,7 +543,7 @@ hipError_t launch_best(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t 
   } else {
     if (whole) consider(cost_of<Tall>(a, q, 256, 115), launch<Tall>);
   }
-  return best(a, q, s);
+  return best(a, q, s, ev);
 }
 
 }  // namespace
@@ -571,15 +572,17 @@ hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, c
   return hipGetLastError();
 }
 
-hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s) {
+hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s, hipEvent_t ev_start,
+                                    hipEvent_t ev_stop) {
+  const LaunchEvents ev{ev_start, ev_stop};
   QuantizedArgs q{};
   q.codes = packed;
   q.scales = static_cast<const char*>(packed) + padded_tiles(a.n) * k_blocks(a.d) * kBlockBytes;
   q.group = group; q.groups = (a.d + group - 1) / group; q.zeros = zeros;
   const int rows = a.B * a.L;
-  if (a.C == 2) return rows <= 8 ? launch_best<2, 1, 8>(a, q, s) : launch_best<2, 1, 32>(a, q, s);
-  if (rows <= 8) return launch_best<1, 1, 8>(a, q, s);
-  return rows <= 32 ? launch_best<1, 1, 32>(a, q, s) : launch_best<1, 2, 32>(a, q, s);
+  if (a.C == 2) return rows <= 8 ? launch_best<2, 1, 8>(a, q, s, ev) : launch_best<2, 1, 32>(a, q, s, ev);
+  if (rows <= 8) return launch_best<1, 1, 8>(a, q, s, ev);
+  return rows <= 32 ? launch_best<1, 1, 32>(a, q, s, ev) : launch_best<1, 2, 32>(a, q, s, ev);
 }
 
 }  // namespace scd

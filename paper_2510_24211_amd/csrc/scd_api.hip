@@ -549,7 +549,10 @@ int scd_step_quantized(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, 
   a.pos = field<int32_t>(c, st, SCD_F_POS);
   a.iter = field<int32_t>(c, st, SCD_F_ITER);
   a.parity_stride = static_cast<size_t>(c->cfg.B) * c->cfg.L * c->n;
-  if (scd::launch_lm_head_quantized(a, W->d_packed, W->group, W->zeros != 0, c->stream) != hipSuccess) return SCD_EHIP;
+  const bool timed = c->ev_start && c->ev_stop;
+  if (scd::launch_lm_head_quantized(a, W->d_packed, W->group, W->zeros != 0, c->stream, timed ? c->ev_start : nullptr,
+                                    timed ? c->ev_stop : nullptr) != hipSuccess)
+    return SCD_EHIP;
   return run_tail(c, st, 0, nullptr);
 }
 

@@ -227,6 +227,7 @@ size_t quantized_bytes(int n, int d, int group, bool zeros);
 hipError_t launch_quantize(const uint16_t* W, int V, int d, int group, uint8_t* codes, uint16_t* scales, uint8_t* zeros, hipStream_t s);
 hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int n, int d, int group, void* packed,
                                  hipStream_t s);
-hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s);
+hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s,
+                                    hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);      // as in launch_lm_head
 
 }  // namespace scd
