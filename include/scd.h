@@ -305,6 +305,11 @@ int scd_pack_quantized(scd_ctx* ctx, const uint8_t* d_codes, const uint16_t* d_s
 int scd_lm_head_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, float* d_z);
 int scd_step_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, void* d_state);
 
+/* scd_lm_head_kernel_name of these two, which launch the same kernel:
+ * lm_head_quantized_kernel<QuantCfg<1 + CFG, blocks of 32 rows, rows of a block that are loaded, column tiles of a wavefront, wavefronts,
+ * of which share k, KB of LDS, of which share columns>, k of a scaling / 16, zero points> (127 characters hold it). */
+int scd_lm_head_quantized_kernel_name(scd_ctx* ctx, int32_t group, int32_t zeros, char* host_buf, size_t cap);
+
 /* ---- the vocabulary table at the model's other end, and what it learns -------------------------
  * The same table W, bf16 bits [V, d] row-major, all pointers 16-byte aligned (d_ids, d_targets and the
  * float arrays 4-byte).  All of them need cfg.d > 0 (up to 2^24); of the rest of the configuration they use what is

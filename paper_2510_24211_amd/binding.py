@@ -92,6 +92,7 @@ def load():
     lib.scd_pack_quantized.argtypes = [vp, vp, vp, vp, i32, vp]
     lib.scd_lm_head_quantized.argtypes = [vp, vp, quantp, vp]
     lib.scd_step_quantized.argtypes = [vp, vp, quantp, vp]
+    lib.scd_lm_head_quantized_kernel_name.argtypes = [vp, i32, i32, ctypes.c_char_p, sz]
     lib.scd_embed.argtypes = [vp, vp, i32, vp, f32, vp]
     lib.scd_embed_window.argtypes = [vp, vp, vp, f32, vp]
     lib.scd_embed_backward_workspace_bytes.restype = sz
@@ -111,7 +112,7 @@ def load():
     for name in ("scd_create", "scd_destroy", "scd_reset", "scd_state_field", "scd_lm_head",
                  "scd_select", "scd_couple_draft", "scd_couple_draft_static", "scd_verify", "scd_step", "scd_step_logits",
                  "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_quantize",
-                 "scd_pack_quantized", "scd_lm_head_quantized", "scd_step_quantized", "scd_embed", "scd_embed_window",
+                 "scd_pack_quantized", "scd_lm_head_quantized", "scd_step_quantized", "scd_lm_head_quantized_kernel_name", "scd_embed", "scd_embed_window",
                  "scd_embed_backward", "scd_cross_entropy", "scd_cross_entropy_backward",
                  "scd_status", "scdw_gather_hidden", "scdw_copy"):
         getattr(lib, name).restype = ctypes.c_int
@@ -348,6 +349,12 @@ class Scd:
         self._check(self.lib.scd_step_quantized(
             self.ctx, _ptr(h, _BF16, c.B * self.C * c.L * c.d, "h"), self._quantized(W),
             _ptr(state, (torch.uint8,), state_bytes(c), "state")), "scd_step_quantized")
+
+    def lm_head_quantized_kernel_name(self, group, zeros):
+        buf = ctypes.create_string_buffer(128)
+        self._check(self.lib.scd_lm_head_quantized_kernel_name(self.ctx, _int32(group, "group"), int(zeros), buf, 128),
+                    "scd_lm_head_quantized_kernel_name")
+        return buf.value.decode()
 
     # -- the vocabulary table at the model's other end, and what it learns ----------
     def _workspace(self, need, what):

@@ -26,6 +26,8 @@
 #include "lm_head_rows.h"
 #include "tile_loads.h"
 
+#include <stdio.h>
+
 namespace scd {
 namespace {
 
@@ -35,6 +37,10 @@ constexpr int kTileCols = 32, kBlockK = 64, kBlockBytes = 1024, kTilesPad = 8;
 template <int C_, int RB_, int HRB_, int NC_, int NW_, int WK_, int KB_, int WR_ = 1>
 struct QuantCfg {
   static constexpr int C = C_, RB = RB_, HRB = HRB_, NC = NC_, NW = NW_, WK = WK_, WR = WR_, LDS = KB_ * 1024;
+  static int name(char* buf, size_t cap, int step, bool zeros) {
+    return snprintf(buf, cap, "lm_head_quantized_kernel<QuantCfg<%d, %d, %d, %d, %d, %d, %d, %d>, %d, %s>", C, RB, HRB, NC, NW, WK, KB_, WR, step,
+                    zeros ? "true" : "false");
+  }
   static constexpr int THREADS = NW * 64, WC = NW / WK / WR, COLTILES = WC * NC, NB = RB * C / WR;
   static constexpr int HROWS = RB * C * HRB;             // h rows per part of k
   static constexpr int HI = WK * HROWS / 8;              // load instructions for the h rows of a step, all parts
@@ -482,25 +488,27 @@ template <class K>
 bool scales_fit(const QuantizedArgs& q) {
   return up(static_cast<int64_t>(K::COLTILES) * q.groups * kTileCols * (q.zeros ? 4 : 2), 1024) <= K::SCALES;
 }
-template <class K, int STEP>
-void launch_step(const LmHeadArgs& a, const QuantizedArgs& q, dim3 grid, int WT, int MT, hipStream_t s, const LaunchEvents& ev) {
-  if (q.zeros) launch_kernel(lm_head_quantized_kernel<K, STEP, true>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
-  else launch_kernel(lm_head_quantized_kernel<K, STEP, false>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
-}
 // Two column tiles per wavefront leave no registers for groups that end inside a block: those have one.
 inline bool whole_blocks(const QuantizedArgs& q) { return q.group % kBlockK == 0; }
-template <class K>
+template <class K, int STEP>
 hipError_t launch(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s, const LaunchEvents& ev) {
   const int64_t tiles = up(a.n, kTileCols) / kTileCols;
   const int WT = static_cast<int>((tiles + K::COLTILES - 1) / K::COLTILES), MT = (a.B * a.L + K::RB * 32 - 1) / (K::RB * 32);
   const dim3 grid((WT + 7) / 8 * 8 * MT);
-  if constexpr (K::NC == 2) {
-    launch_step<K, 4>(a, q, grid, WT, MT, s, ev);
-  } else {
-    if (whole_blocks(q)) launch_step<K, 4>(a, q, grid, WT, MT, s, ev);
-    else launch_step<K, 2>(a, q, grid, WT, MT, s, ev);
-  }
+  if (q.zeros) launch_kernel(lm_head_quantized_kernel<K, STEP, true>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
+  else launch_kernel(lm_head_quantized_kernel<K, STEP, false>, grid, dim3(K::THREADS), s, ev, a, q, WT, MT);
   return hipGetLastError();
+}
+// The instances for groups of whole blocks and for others.
+struct Kernel {
+  hipError_t (*launch)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t, const LaunchEvents&);
+  int (*name)(char*, size_t, int, bool);
+  int step;
+};
+template <class K>
+Kernel kernel_of(const QuantizedArgs& q) {
+  if constexpr (K::NC == 2) return {launch<K, 4>, K::name, 4};
+  else return whole_blocks(q) ? Kernel{launch<K, 4>, K::name, 4} : Kernel{launch<K, 2>, K::name, 2};
 }
 static_assert(QuantCfg<2, 1, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4 && QuantCfg<1, 2, 32, 1, 4, 4, 160>::SCALES >= kMaxGroups * kTileCols * 4,
               "the scales of one column tile always fit");
@@ -519,31 +527,41 @@ int64_t cost_of(const LmHeadArgs& a, const QuantizedArgs& q, int resident, int r
   return (groups * row_tiles + resident - 1) / resident * round;
 }
 template <int C, int RB, int HRB>
-hipError_t launch_best(const LmHeadArgs& a, const QuantizedArgs& q, hipStream_t s, const LaunchEvents& ev) {
+Kernel best_of(const LmHeadArgs& a, const QuantizedArgs& q) {
   using Four = QuantCfg<C, RB, HRB, 1, 4, 4, 160>;
   using Two = QuantCfg<C, RB, HRB, 1, 8, 2, 160>;
   using One = QuantCfg<C, RB, HRB, 1, 8, 1, 160>;
   using Wide = QuantCfg<C, RB, HRB, 2, 8, 2, 160>;
   using Tall = QuantCfg<C, 8 / C, 32, 2, 8, 1, 160, 4>;          // a quarter of 256 rows per wavefront
   const bool whole = whole_blocks(q);
-  hipError_t (*best)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t, const LaunchEvents&) = launch<Four>;
+  Kernel best = kernel_of<Four>(q);
   int64_t least = cost_of<Four>(a, q, 256, HRB == 8 ? 13 : 29);
-  auto consider = [&](int64_t cost, hipError_t (*f)(const LmHeadArgs&, const QuantizedArgs&, hipStream_t, const LaunchEvents&)) {
+  auto consider = [&](int64_t cost, Kernel k) {
     if (cost < least) {
       least = cost;
-      best = f;
+      best = k;
     }
   };
-  consider(cost_of<Two>(a, q, 256, HRB == 8 ? 23 : 35), launch<Two>);
-  consider(cost_of<One>(a, q, 256, HRB == 8 ? 40 : 57), launch<One>);
-  if (whole) consider(cost_of<Wide>(a, q, 256, HRB == 8 ? 31 : 51), launch<Wide>);
+  consider(cost_of<Two>(a, q, 256, HRB == 8 ? 23 : 35), kernel_of<Two>(q));
+  consider(cost_of<One>(a, q, 256, HRB == 8 ? 40 : 57), kernel_of<One>(q));
+  if (whole) consider(cost_of<Wide>(a, q, 256, HRB == 8 ? 31 : 51), kernel_of<Wide>(q));
   if constexpr (HRB == 8) {
     using Small = QuantCfg<C, RB, HRB, 1, 4, 4, 80>;             // two of them per CU
-    consider(cost_of<Small>(a, q, 512, 15), launch<Small>);
+    consider(cost_of<Small>(a, q, 512, 15), kernel_of<Small>(q));
   } else {
-    if (whole) consider(cost_of<Tall>(a, q, 256, 115), launch<Tall>);
+    if (whole) consider(cost_of<Tall>(a, q, 256, 115), kernel_of<Tall>(q));
   }
-  return best(a, q, s, ev);
+  return best;
+}
+Kernel kernel_for(const LmHeadArgs& a, const QuantizedArgs& q) {
+  const int rows = a.B * a.L;
+  if (a.C == 2) return rows <= 8 ? best_of<2, 1, 8>(a, q) : best_of<2, 1, 32>(a, q);
+  if (rows <= 8) return best_of<1, 1, 8>(a, q);
+  return rows <= 32 ? best_of<1, 1, 32>(a, q) : best_of<1, 2, 32>(a, q);
+}
+QuantizedArgs quantized_args(const LmHeadArgs& a, const void* packed, int group, bool zeros) {
+  const char* const codes = static_cast<const char*>(packed);
+  return {codes, codes ? codes + padded_tiles(a.n) * k_blocks(a.d) * kBlockBytes : nullptr, group, (a.d + group - 1) / group, zeros};
 }
 
 }  // namespace
@@ -574,15 +592,13 @@ hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, c
 
 hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s, hipEvent_t ev_start,
                                     hipEvent_t ev_stop) {
-  const LaunchEvents ev{ev_start, ev_stop};
-  QuantizedArgs q{};
-  q.codes = packed;
-  q.scales = static_cast<const char*>(packed) + padded_tiles(a.n) * k_blocks(a.d) * kBlockBytes;
-  q.group = group; q.groups = (a.d + group - 1) / group; q.zeros = zeros;
-  const int rows = a.B * a.L;
-  if (a.C == 2) return rows <= 8 ? launch_best<2, 1, 8>(a, q, s, ev) : launch_best<2, 1, 32>(a, q, s, ev);
-  if (rows <= 8) return launch_best<1, 1, 8>(a, q, s, ev);
-  return rows <= 32 ? launch_best<1, 1, 32>(a, q, s, ev) : launch_best<1, 2, 32>(a, q, s, ev);
+  const QuantizedArgs q = quantized_args(a, packed, group, zeros);
+  return kernel_for(a, q).launch(a, q, s, LaunchEvents{ev_start, ev_stop});
+}
+
+int lm_head_quantized_kernel_name(const LmHeadArgs& a, int group, bool zeros, char* buf, size_t cap) {
+  const Kernel k = kernel_for(a, quantized_args(a, nullptr, group, zeros));
+  return k.name(buf, cap, k.step, zeros);
 }
 
 }  // namespace scd

@@ -556,6 +556,13 @@ int scd_step_quantized(scd_ctx* c, const uint16_t* d_h, const scd_quantized* W, 
   return run_tail(c, st, 0, nullptr);
 }
 
+int scd_lm_head_quantized_kernel_name(scd_ctx* c, int32_t group, int32_t zeros, char* host_buf, size_t cap) {
+  if (!c || !host_buf || !valid_group(c->cfg, group) || (zeros != 0 && zeros != 1)) return SCD_EINVAL;
+  scd::LmHeadArgs a{};
+  a.B = c->cfg.B; a.C = c->C; a.L = c->cfg.L; a.d = c->cfg.d; a.n = c->n;
+  return static_cast<size_t>(scd::lm_head_quantized_kernel_name(a, group, zeros != 0, host_buf, cap)) >= cap ? SCD_EINVAL : SCD_OK;
+}
+
 // ---- operators on the vocabulary table ---------------------------------------------------
 size_t scd_embed_backward_workspace_bytes(const scd_config* cfg, int32_t rows) {
   if (!valid_config(cfg) || cfg->d <= 0 || cfg->d > kEmbedWidth || rows < 0 || rows > kEmbedRows) return 0;

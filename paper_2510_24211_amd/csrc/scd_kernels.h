@@ -229,5 +229,7 @@ hipError_t launch_pack_quantized(const uint8_t* codes, const uint16_t* scales, c
                                  hipStream_t s);
 hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int group, bool zeros, hipStream_t s,
                                     hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);      // as in launch_lm_head
+// Name of the kernel that it picks (B, C, L, d and n are read); snprintf semantics.
+int lm_head_quantized_kernel_name(const LmHeadArgs& a, int group, bool zeros, char* buf, size_t cap);
 
 }  // namespace scd
