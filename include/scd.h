@@ -365,6 +365,12 @@ int scd_cross_entropy_backward(scd_ctx* ctx, const uint16_t* d_h, const uint16_t
                                const float* d_lse, const float* d_weight, uint16_t* d_dh, void* d_dW, int32_t grad_type,
                                int32_t accumulate, void* d_workspace, size_t workspace_bytes);
 
+/* For reports: the kernels of both calls' matrix products for `rows` rows, gemm_kernel<rows of a tile, columns of a tile, use>, and how many
+ * ids the gradient takes at a time (the last piece may have fewer), NUL-terminated, in host_buf[0..cap): "gemm_kernel<.., kLoss>; pieces of
+ * N: gemm_kernel<.., kGradient>, gemm_kernel<.., kRows> in K parts, gemm_kernel<.., kTable or kTableTwoTerms>" (255 characters
+ * hold it).  SCD_OK, or SCD_EINVAL / SCD_EUNSUPPORTED as the calls.  Host-only call. */
+int scd_cross_entropy_kernel_names(scd_ctx* ctx, int32_t rows, int32_t grad_type, char* host_buf, size_t cap);
+
 /* Synchronises the stream and reports: host_flags[0] = numeric-fault bits,
  * host_flags[1] = 1 if every sequence has emitted N tokens, host_flags[2] =
  * largest t_b, host_flags[3] = 0.  Returns SCD_ENUMERIC if a fault bit is set. */

@@ -104,6 +104,7 @@ def load():
     lib.scd_cross_entropy_backward_workspace_bytes.restype = sz
     lib.scd_cross_entropy_backward_workspace_bytes.argtypes = [cfgp, i32, i32]
     lib.scd_cross_entropy_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, sz]
+    lib.scd_cross_entropy_kernel_names.argtypes = [vp, i32, i32, ctypes.c_char_p, sz]
     lib.scd_status.argtypes = [vp, vp, ctypes.POINTER(i32 * 4)]
     lib.scd_strerror.restype = ctypes.c_char_p
     lib.scd_strerror.argtypes = [ctypes.c_int]
@@ -114,7 +115,7 @@ def load():
                  "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_quantize",
                  "scd_pack_quantized", "scd_lm_head_quantized", "scd_step_quantized", "scd_lm_head_quantized_kernel_name", "scd_embed", "scd_embed_window",
                  "scd_embed_backward", "scd_cross_entropy", "scd_cross_entropy_backward",
-                 "scd_status", "scdw_gather_hidden", "scdw_copy"):
+                 "scd_cross_entropy_kernel_names", "scd_status", "scdw_gather_hidden", "scdw_copy"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -414,6 +415,12 @@ class Scd:
             _ptr(dW, tuple(_GRAD), c.V * c.d, "dW"), _grad_type(dW.dtype) if dW is not None else GRAD_BF16,
             int(accumulate), _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()),
             "scd_cross_entropy_backward")
+
+    def cross_entropy_kernel_names(self, rows, grad_dtype=torch.bfloat16):
+        buf = ctypes.create_string_buffer(256)
+        self._check(self.lib.scd_cross_entropy_kernel_names(self.ctx, _int32(rows, "rows"), _grad_type(grad_dtype), buf, 256),
+                    "scd_cross_entropy_kernel_names")
+        return buf.value.decode()
 
     # -- benchmark plumbing ---------------------------------------------------
     def gather_hidden(self, table, age_cap, state, h):

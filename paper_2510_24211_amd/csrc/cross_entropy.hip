@@ -23,6 +23,8 @@
 #include "scd_device.h"
 #include "scd_kernels.h"
 
+#include <stdio.h>
+
 namespace scd {
 namespace {
 
@@ -611,6 +613,15 @@ hipError_t launch_cross_entropy(const CrossEntropyArgs& c, hipStream_t s) {
   hipLaunchKernelGGL(finish_kernel, dim3((c.rows + 3) / 4), dim3(256), 0, s, a.part, a.zt, c.targets, c.rows, c.n, (c.n + bn - 1) / bn,
                      a.scale2, a.inv_tau, c.loss, c.lse);
   return hipGetLastError();
+}
+
+int cross_entropy_kernel_names(int rows, int n, int d, bool f32, char* buf, size_t cap) {
+  const Plan p = make_plan(rows, n, d, f32);
+  const Shape l = choose(rows, n), g = choose(rows, p.piece), r = choose(rows, d), t = choose(p.piece, d);
+  return snprintf(buf, cap,
+                  "gemm_kernel<%d, %d, kLoss>; pieces of %d: gemm_kernel<%d, %d, kGradient>, gemm_kernel<%d, %d, kRows> in %d parts, "
+                  "gemm_kernel<%d, %d, %s>",
+                  l.hr, l.bn, p.piece, g.hr, g.bn, r.hr, r.bn, p.parts, t.hr, t.bn, f32 ? "kTableTwoTerms" : "kTable");
 }
 
 size_t cross_entropy_backward_bytes(int rows, int n, int d, bool f32) { return make_plan(rows, n, d, f32).total; }

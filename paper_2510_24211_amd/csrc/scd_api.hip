@@ -649,6 +649,13 @@ int scd_cross_entropy_backward(scd_ctx* c, const uint16_t* d_h, const uint16_t* 
   return hip_rc(scd::launch_cross_entropy_backward(a, c->stream));
 }
 
+int scd_cross_entropy_kernel_names(scd_ctx* c, int32_t rows, int32_t grad_type, char* host_buf, size_t cap) {
+  if (!c || !host_buf || rows < 0 || rows > kCrossEntropyRows || !valid_gradient(grad_type, 0) || c->cfg.d <= 0) return SCD_EINVAL;
+  if (c->C != 1 || !cross_entropy_fits(rows, c->n, c->cfg.d, c->cfg.temperature)) return SCD_EUNSUPPORTED;
+  const int len = scd::cross_entropy_kernel_names(rows, c->n, c->cfg.d, grad_type == SCD_GRAD_F32, host_buf, cap);
+  return static_cast<size_t>(len) >= cap ? SCD_EINVAL : SCD_OK;
+}
+
 int scd_status(scd_ctx* c, void* st, int32_t host_flags[4]) {
   if (!c || !st || !host_flags) return SCD_EINVAL;
   const int B = c->cfg.B;

@@ -214,6 +214,8 @@ size_t cross_entropy_bytes(int rows, int n, int d);
 hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t s);
 size_t cross_entropy_backward_bytes(int rows, int n, int d, bool f32);
 hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& a, hipStream_t s);
+// The matrix products of both for these sizes; snprintf semantics.
+int cross_entropy_kernel_names(int rows, int n, int d, bool f32, char* buf, size_t cap);
 
 // The LM head over 4-bit weights, laid out by launch_pack_quantized.  Of LmHeadArgs it reads what z and the rows of h need.
 struct QuantizedArgs {
