@@ -594,7 +594,7 @@ Plan make_plan(int rows, int n, int d, bool f32) {
 
 }  // namespace
 
-size_t cross_entropy_bytes(int rows, int n, int) {
+size_t cross_entropy_bytes(int rows, int n) {
   const size_t tiles = (static_cast<size_t>(n) + 63) / 64;           // the narrowest tile's
   return up256(sizeof(float2) * tiles * rows) + up256(sizeof(float) * rows) + 256;
 }

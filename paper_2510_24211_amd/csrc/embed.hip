@@ -14,13 +14,12 @@
 // 16 of them the zeros' bytes).  The lookup of 25600 rows takes 66 us, of 64 rows 5.4, a launch.
 #include "scd_device.h"
 #include "scd_kernels.h"
+#include "tile_loads.h"
 
 namespace scd {
 namespace {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x8 widen(u32x4 v) { return __builtin_convertvector(__builtin_bit_cast(bf16x8, v), f32x8); }
 __device__ __forceinline__ u32x4 narrow(f32x8 v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)); }
@@ -107,9 +106,9 @@ __device__ __forceinline__ void count_digits(const uint32_t (&k)[ROUNDS], const 
     const uint64_t same = equal_digits(digit, g.bits, live);
     const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
     place[j] = mine[digit] + before;
-    asm volatile("" ::: "memory");       // LDS operations of a wavefront are performed in order
+    compiler_fence();                     // LDS operations of a wavefront are performed in order
     if (is && before == 0u) mine[digit] += __popcll(same);
-    asm volatile("" ::: "memory");
+    compiler_fence();
   }
   __syncthreads();
 }
@@ -400,7 +399,6 @@ __global__ __launch_bounds__(256) void sum_kernel(const SumArgs a) {
 constexpr int kJoinWaves = 8;
 template <bool F32, bool ACC>
 __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(const SumArgs a) {
-  constexpr int split = kJoinWaves;
   __shared__ f32x8 sums[kJoinWaves][64];
   __shared__ int run[kJoinWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -426,22 +424,22 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_kernel(const SumArgs a) 
     last += n;
     if (n < kJoinWaves * 64) break;
   }
-  const int first = chunk + 1, count = last - first + 1, per = (count + split - 1) / split, share = wave;
-  const int c0 = first + share * per, c1 = min(c0 + per, last + 1);
+  const int first = chunk + 1, count = last - first + 1, per = (count + kJoinWaves - 1) / kJoinWaves;
+  const int c0 = first + wave * per, c1 = min(c0 + per, last + 1);
   const int col = blockIdx.y * kSlice + lane * 8;
   const bool mine = col < a.d;
   f32x8 sum{};
   if (mine) {
     const float* const at = a.part + col;
-    if (share == 0) sum = *reinterpret_cast<const f32x8*>(at + (static_cast<int64_t>(chunk) * 2 + 1) * a.d);
+    if (wave == 0) sum = *reinterpret_cast<const f32x8*>(at + (static_cast<int64_t>(chunk) * 2 + 1) * a.d);
 #pragma unroll 8
     for (int c = c0; c < c1; ++c) sum += *reinterpret_cast<const f32x8*>(at + static_cast<int64_t>(c) * 2 * a.d);
   }
   sums[wave][lane] = sum;
   __syncthreads();
-  if (share != 0 || !mine) return;
+  if (wave != 0 || !mine) return;
 #pragma unroll
-  for (int w = 1; w < split; ++w) sum += sums[wave + w][lane];
+  for (int w = 1; w < kJoinWaves; ++w) sum += sums[w][lane];
   put<F32, ACC>(a.dW, key, a.d, col, sum * a.scale);
 }
 

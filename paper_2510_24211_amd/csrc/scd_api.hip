@@ -611,7 +611,7 @@ int scd_embed_backward(scd_ctx* c, const int32_t* d_ids, int32_t rows, const uin
 
 size_t scd_cross_entropy_workspace_bytes(const scd_config* cfg, int32_t rows) {
   if (!valid_config(cfg) || cfg->d <= 0 || rows < 0 || rows > kCrossEntropyRows || !cross_entropy_fits(rows, cfg->v_hi - cfg->v_lo, cfg->d, cfg->temperature)) return 0;
-  return scd::cross_entropy_bytes(rows, cfg->v_hi - cfg->v_lo, cfg->d);
+  return scd::cross_entropy_bytes(rows, cfg->v_hi - cfg->v_lo);
 }
 
 size_t scd_cross_entropy_backward_workspace_bytes(const scd_config* cfg, int32_t rows, int32_t grad_type) {
@@ -626,7 +626,7 @@ int scd_cross_entropy(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, cons
   if (!c || (rows > 0 && (!d_loss || !d_lse)) || !aligned(d_loss, 4) || !aligned(d_lse, 4)) return SCD_EINVAL;
   scd::CrossEntropyArgs a{};
   if (int rc = cross_entropy_args(c, d_h, d_W, d_targets, rows, &a); rc != SCD_OK) return rc;
-  if (!valid_workspace(d_workspace, workspace_bytes, scd::cross_entropy_bytes(rows, c->n, c->cfg.d))) return SCD_EWORKSPACE;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::cross_entropy_bytes(rows, c->n))) return SCD_EWORKSPACE;
   a.loss = d_loss; a.lse = d_lse; a.ws = d_workspace;
   return hip_rc(scd::launch_cross_entropy(a, c->stream));
 }

@@ -210,7 +210,7 @@ struct CrossEntropyArgs {
   bool f32, accumulate;
   void* ws;                  // cross_entropy_bytes / cross_entropy_backward_bytes, 256-byte aligned
 };
-size_t cross_entropy_bytes(int rows, int n, int d);
+size_t cross_entropy_bytes(int rows, int n);
 hipError_t launch_cross_entropy(const CrossEntropyArgs& a, hipStream_t s);
 size_t cross_entropy_backward_bytes(int rows, int n, int d, bool f32);
 hipError_t launch_cross_entropy_backward(const CrossEntropyArgs& a, hipStream_t s);
