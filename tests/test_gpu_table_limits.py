@@ -65,3 +65,109 @@ def test_a_packed_table_of_64_gib():
     assert not z[0, 0, rest].any()
     del codes, W, z, rest
     torch.cuda.empty_cache()
+
+
+def _whole(g, *shape):
+    """Small whole numbers: sums of them are exact in fp32, whatever the order."""
+    return torch.randint(-3, 4, shape, device="cuda", generator=g).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows,V,d", [(3, 5, 1 << 24), (1 << 25, 40, 8), (1000, (1 << 31) - 1, 8)])
+def test_embedding_and_gradient_at_the_largest_sizes(rows, V, d):
+    """Whole numbers: the looked-up rows times 2 and the gradient of as many rows of one id as there are (up to 2^24) are exact; bf16 rounds once."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    s = B.Scd(B.make_config(B=1, L=1, N=1, V=V, d=d))
+    ids = torch.randint(max(0, V - 700), V, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    ids[:3] = torch.tensor([0, V - 1, -1], dtype=torch.int32)
+    low = max(0, V - 700)
+    W = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    W[0], W[low:] = 3.0, _whole(g, V - low, d)
+    x = torch.full((rows, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    s.embed(ids, W, 2.0, x)
+    there = ids >= 0
+    for a in range(0, rows, 1 << 22):
+        b = min(a + (1 << 22), rows)
+        want = torch.where(there[a:b, None], W[ids[a:b].clamp(min=0).long()] * 2, 0)
+        assert torch.equal(x[a:b], want)
+    dx = x.copy_(_whole(g, rows, d))
+    dW = W.fill_(7.0)
+    s.embed_backward(ids, dx, 1.0, dW, s.embed_backward_workspace(rows))
+    want = torch.zeros(V - low, d, device="cuda")
+    far = there & (ids >= low)
+    want.index_add_(0, (ids[far] - low).long(), dx[far].float())
+    assert torch.equal(dW[low:], want.to(torch.bfloat16))
+    if low > 0:
+        assert torch.equal(dW[0].float(), dx[0].float())
+        for a in range(1, low, 1 << 28):
+            assert not dW[a:min(a + (1 << 28), low)].any()
+    del W, x, dx, dW
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,n,d", [(3, 40, 1 << 21), (130, 300, 1 << 21), (1 << 20, 70, 8), (1 << 20, 300, 72)])
+def test_cross_entropy_at_the_largest_sizes(rows, n, d):
+    """Rows that hold one number each: h_r = a_r e_(k_r), so that a logit is one product, W has whole numbers / 2, and
+    the gradients are dh_r = (p - hot) W and dW = (p - hot)^T h.  dz errs by p times twice the logits' and lse's errors (64 u (1 + |z|)) and by
+    2^-11 of itself or 2^-39 of 1; sums in one chain of `rows` or n terms with a margin of 4; the result by half a step."""
+    g = torch.Generator(device="cuda").manual_seed(rows + d)
+    s = B.Scd(B.make_config(B=1, L=1, N=1, V=n, d=d))
+    W = (_whole(g, n, d).float() / 2).to(torch.bfloat16)
+    k = torch.randint(0, d, (rows,), device="cuda", generator=g)
+    k[0], k[-1] = d - 1, 0
+    h = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    r = torch.arange(rows, device="cuda")
+    h[r, k] = _whole(g, rows)
+    a = h[r, k].double()
+    t = torch.randint(-1, n, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    s.cross_entropy(h, W, t, loss, lse, s.cross_entropy_workspace(rows))
+    dh, dW = torch.empty_like(h), torch.empty_like(W)
+    s.cross_entropy_backward(h, W, t, lse, None, dh, dW, s.cross_entropy_backward_workspace(rows))
+    z = a[:, None] * W[:, k].t().double()
+    want = torch.logsumexp(z, 1)
+    assert ((lse.double() - want).abs() <= 64 * U * (1 + z.abs().amax(1))).all()
+    dz = torch.softmax(z, 1)
+    there = (t >= 0).nonzero()[:, 0]
+    dz[there, t[there].long()] -= 1
+    dz[t < 0] = 0
+    e = (128 * U * (1 + z.abs().amax(1, keepdim=True)) + 2.0 ** -11) * dz.abs() + 64 * U * (dz < 0) + 2.0 ** -39
+    # dW by its columns: the rows that hold a number there
+    cols = k.unique()[:2000]
+    at = torch.searchsorted(cols, k).clamp(max=len(cols) - 1)
+    mine = cols[at] == k
+    wanted, bound = (torch.zeros(len(cols), n, dtype=torch.float64, device="cuda") for _ in range(2))
+    wanted.index_add_(0, at[mine], a[mine, None] * dz[mine])
+    bound.index_add_(0, at[mine], a[mine, None].abs() * (e[mine] + 4 * math.sqrt(rows) * U * dz[mine].abs()))
+    got = dW[:, cols].t().double()
+    assert ((got - wanted).abs() <= bound + 2.0 ** -8 * (wanted.abs() + bound)).all()
+    rest = torch.ones(d, dtype=torch.bool, device="cuda")
+    rest[k] = False
+    assert not dW[:, rest].any()
+    for lo in range(0, d, 1 << 15):
+        w = W[:, lo:lo + (1 << 15)].double()
+        wanted, bound = dz @ w, (e + 4 * math.sqrt(n) * U * dz.abs()) @ w.abs()
+        got = dh[:, lo:lo + (1 << 15)].double()
+        assert ((got - wanted).abs() <= bound + 2.0 ** -8 * (wanted.abs() + bound)).all(), lo
+
+
+@pytest.mark.parametrize("lam,L,n", [(0.0, 256, 70), (3.0, 130, 40)])
+def test_quantized_head_over_the_longest_rows(lam, L, n):
+    """2^20 weights a row, 256 groups: whole numbers times powers of two, exact."""
+    d, group = 1 << 20, 4096
+    g = torch.Generator(device="cuda").manual_seed(5)
+    s = B.Scd(B.make_config(B=2, L=L, N=L, V=n, d=d, cfg_lambda=lam))
+    codes = torch.randint(0, 256, (n, d // 2), device="cuda", generator=g, dtype=torch.uint8)
+    scales = torch.where(torch.rand(n, 256, device="cuda", generator=g) < 0.5, 0.5, 1.0).to(torch.bfloat16)
+    zp = torch.randint(0, 16, (n, 256), device="cuda", generator=g, dtype=torch.uint8)
+    h = torch.zeros(2, s.C, L, d, dtype=torch.bfloat16, device="cuda")
+    h[..., :64] = _whole(g, 2, s.C, L, 64)
+    h[..., -4100:-4000] = _whole(g, 2, s.C, L, 100)
+    h[..., d // 2] = 2
+    z = torch.empty(2, L, n, device="cuda")
+    s.lm_head_quantized(h, s.pack_quantized(codes, scales, zp, group), z)
+    q = torch.stack([codes & 15, codes >> 4], 2).reshape(n, 256, group).float()
+    W = (scales.float()[:, :, None] * (q - zp.float()[:, :, None])).reshape(n, d)
+    used = torch.cat([torch.arange(64), torch.arange(d - 4100, d - 4000), torch.tensor([d // 2])]).cuda()
+    a = h[..., used].double() @ W[:, used].double().t()
+    want = (1 + lam) * a[:, 0] - lam * a[:, -1]
+    assert torch.equal(z.double(), want)
