@@ -301,7 +301,8 @@ int scd_pack_quantized(scd_ctx* ctx, const uint8_t* d_codes, const uint16_t* d_s
                        void* d_packed);
 
 /* scd_lm_head and scd_step with these weights in the place of W.  The products are exact and summed in fp32: no weight is
- * rounded to bf16. */
+ * rounded to bf16.  Meant for few rows on large tables, in groups of 64 or more; batches of some hundred rows, and groups of 32 with zero
+ * points, take longer than over W in bf16. */
 int scd_lm_head_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, float* d_z);
 int scd_step_quantized(scd_ctx* ctx, const uint16_t* d_h, const scd_quantized* W, void* d_state);
 
@@ -314,7 +315,8 @@ int scd_lm_head_quantized_kernel_name(scd_ctx* ctx, int32_t group, int32_t zeros
  * The same table W, bf16 bits [V, d] row-major, all pointers 16-byte aligned (d_ids, d_targets and the
  * float arrays 4-byte).  All of them need cfg.d > 0 (up to 2^24); of the rest of the configuration they use what is
  * named below, so a context with B = L = N = 1 serves a program that decodes nothing.  `rows` = 0 is allowed (arrays of
- * no elements may then be NULL), up to 2^25 ids or 2^20 rows of the loss.  Workspaces are the caller's, 256-byte aligned, of the size that the
+ * no elements may then be NULL), up to 2^25 ids (the gradient of more than 2^20 takes a time that grows with their square) or 2^20 rows
+ * of the loss.  Workspaces are the caller's, 256-byte aligned, of the size that the
  * query gives for the same arguments (0 for bad ones); nothing in one outlives the call.  Calls on different
  * streams, contexts or in different recorded graphs must not share one if they may overlap in time. */
 

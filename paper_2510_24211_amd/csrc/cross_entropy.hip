@@ -16,9 +16,9 @@
 // dz enters its product as two terms, at the price of a fifth product: what the first one leaves, times 2^11, has sums of its own, which
 // are brought down again before the first terms' are added to them.  So dz errs by 2^-22 of itself or 2^-50 of the largest
 // weight, whichever is more.  Statistics and sums are fp32.
-//   Bound by the matrix pipes: 4096 rows x 65536 ids over 4096 take 7.8 ms, the four products at 1.15 to 1.25 PFLOP/s (6.2 ms at the 1.42
-// of a large library product), turning W 220 us, its largest element 108, dh's sums over the pieces about 100; the forward pass of 2304 rows
-// 1.06 ms (1.17 PFLOP/s).  Few rows are bound by W: 77 x 16384 over 1280 16.6 us, 42 MB.
+//   Bound by the matrix pipes: 4096 rows x 65536 ids over 4096 take 7.6 to 7.9 ms, the four products at 1.1 to 1.25 PFLOP/s (6.2 ms at the 1.42
+// of a large library product), turning W 212 us, its largest element 98, dh's sums over the pieces about 100; the forward pass of 2304 rows
+// 1.05 to 1.1 ms (1.13 to 1.18 PFLOP/s).  Few rows are bound by W: 77 x 16384 over 1280 16.5 to 17.5 us, 42 MB.
 #include "gemm_tile.h"
 #include "scd_device.h"
 #include "scd_kernels.h"

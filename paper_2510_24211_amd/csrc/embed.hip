@@ -12,6 +12,9 @@
 //   Bound by memory where there is much to move: 25600 rows of 4096 (a fifth in one id) on 64000 ids take 189 us, 150 of them in the sums'
 // launch (4.9 TB/s), 31 for sorting and 7.5 for joining; by its three launches where there is not (576 rows of 1280 on 16384 ids, fp32: 33 us,
 // 16 of them the zeros' bytes).  The lookup of 25600 rows takes 66 us, of 64 rows 5.4, a launch.
+//   In sorting, every block of 2048 rows reads the digits' counts of all blocks: a term that grows with the square of the rows.  It is lost in the
+// rest up to some 2^20 rows (all of the gradient for rows of 8 columns: 186 us for 2^20 rows, 0.75 ms for 2^22) and is nearly all there is at the
+// limit of 2^25 (21 ms).
 #include "scd_device.h"
 #include "scd_kernels.h"
 #include "tile_loads.h"

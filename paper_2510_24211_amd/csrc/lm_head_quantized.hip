@@ -7,8 +7,8 @@
 //   sum over a group of h * (q - o) = sum h * (16 + q) - (16 + o) * sum h.
 // The second sum is taken once per workgroup, by whoever loaded the rows.  It goes to the matrix units too, split into three
 // bf16 terms of 8 bits each that hold all 24, times -(16 + o), which bf16 holds: one more MFMA for each four (C operands of that
-// value would cost four times the LDS reads).  At a group's end the accumulators are scaled and added to the fp32 logits: no
-// weight is ever rounded.
+// value would cost four times the LDS reads).  After every block of 64 k, or half of one where groups end inside, the accumulators are scaled
+// and added to the fp32 logits, whatever the group's length: no weight is ever rounded.
 //
 // Layout.  Columns in tiles of 32, k in blocks of 64: a block of a tile is 1 KB, 16 bytes for each lane of a wavefront, which
 // are its operands of four 32x32x16 MFMAs (lane l: column l % 32; word j: k = 16 j + 8 (l / 32) + 0 .. 7, even k in
@@ -19,9 +19,12 @@
 // rows and take 1/WK of k each (their sums are added up at the end in a fixed order), WR share tiles and take a part of the rows
 // each.  Weights and h rows go from memory straight into LDS, S stages deep.  The scales of the workgroup's columns are fetched whole at
 // the start.
-//   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096 take 54 us, of which the loads alone would take 25 to 30 (142 MB); a
-// wavefront issues about 220 vector instructions per step of two tiles (64 convert codes, 64 scale, 30 add rows up) beside 20 MFMAs, and the
+//   Bound by instruction issue: 32 rows with guidance x 65536 ids over 4096, groups of 128, take 54 to 58 us, of which the loads alone would take
+// 25 to 30 (142 MB); a wavefront issues about 220 vector instructions per step of two tiles (64 convert codes, 64 scale, 30 add rows up) beside 20 MFMAs, and the
 // matrix pipes are busy a quarter of the time.  With the offsets taken off by a product with ones it took 75, as C operands from LDS 63.
+// The bf16 head takes 82 there.  Shorter groups bring more scales, which shut out the faster shapes of workgroups: groups of 64 take 64 us, with zero points
+// 75, of 32 83, with zero points 231.  Batches are slower than the bf16 head too (480 rows with guidance x 8191: 114 to 117 us against 60):
+// codes are converted by each of the four wavefronts that share columns.
 #include "launch_events.h"
 #include "lm_head_rows.h"
 #include "tile_loads.h"
@@ -401,7 +404,9 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_quantized_kernel(const LmH
 
 // ---- quantisation and layout ---------------------------------------------------------------------------
 // A wavefront per row and group.  Without zero points s = max(largest / 7, -smallest / 8), with them s = (largest -
-// smallest) / 15 over a range that holds 0; s is rounded to bf16 first, the codes are the nearest under the rounded one.
+// smallest) / 15 over a range that holds 0; s is rounded to bf16 first, the codes are the nearest under the rounded one.  Once per table, and
+// not tuned: 65536 x 4096 in groups of 128 580 to 630 us, of 64 1130, of 32 2000 (two passes over the group, 4 bytes per lane and load, a
+// division per weight; 0.67 GB, 131 us at a copy's rate).
 __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restrict__ W, int64_t items, int d, int group, int groups,
                                                        uint8_t* __restrict__ codes, uint16_t* __restrict__ scales, uint8_t* __restrict__ zeros) {
   const int lane = threadIdx.x & 63;
@@ -440,7 +445,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(const uint16_t* __restric
   }
 }
 
-// A wavefront per column tile and block of k: 16 bytes per lane.  (Tables of 64 GiB have more of them than a launch has threads for.)
+// A wavefront per column tile and block of k: 16 bytes per lane.  Once per table: 65536 x 4096 90 to 100 us (52 at a copy's rate; a lane gathers
+// 4 bytes from each of four places of its row), the scales 8.  (Tables of 64 GiB have more of them than a launch has threads for.)
 __global__ __launch_bounds__(256) void pack_codes_kernel(const uint8_t* __restrict__ codes, int n, int d, int KB, int64_t blocks,
                                                          u32x4* __restrict__ to) {
   const int lane = threadIdx.x & 63;
