@@ -517,12 +517,12 @@ struct Shape {
 // Tiles by what one round of a workgroup per CU costs, relative to each other as the LM head's were measured.  2304 rows x 8192 ids over 4096
 // (288 tiles of 256 x 256) take 194 us in 387 tiles of 256 x 192, 201 in 576 of 256 x 128; the 144 tiles of dh's product there 212
 // us, 198 of 256 x 192 176; 77 rows x 16384 ids over 1280 18.7 us in 128 tiles of 128 x 128, 15.2 in 256 of 128 x 64.
-// A launch holds fewer than 2^32 threads: 2^30 ids are too many tiles of 128 columns.
+// A launch holds fewer than 2^32 threads: 2^30 ids are too many tiles of 128 columns.  (What is too many of any fits no memory either.)
 constexpr int64_t kMostTiles = (1 << 23) - 8;
 Shape choose(int64_t M, int64_t N) {
   struct Option { int hr, bn, cost; };
   constexpr Option options[] = {{128, 64, 18}, {128, 128, 27}, {256, 128, 40}, {256, 192, 56}, {256, 256, 73}};
-  Shape best{};
+  Shape best{256, 256};
   int64_t least = -1;
   for (const Option& o : options) {
     const int64_t tiles = (M + o.hr - 1) / o.hr * ((N + o.bn - 1) / o.bn), cost = (tiles + 255) / 256 * o.cost;
