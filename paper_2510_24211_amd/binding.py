@@ -219,6 +219,8 @@ class Scd:
 
     def _empty(self, nbytes):
         """Memory of the context's stream: what another stream has freed may be in use there still."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
