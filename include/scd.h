@@ -159,7 +159,7 @@ typedef enum scd_field {
 } scd_field;
 
 /* Bytes of caller-provided device scratch a context needs; 0 on a bad config.  Nothing in it outlives
- * a call.  scd_couple_draft writes it, and so do scd_select, scd_step, scd_step_quantized and scd_step_logits where a
+ * a call.  scd_couple_draft writes it, and so do scd_select, scd_step, scd_step_quantized, scd_step_fp8 and scd_step_logits where a
  * top-k of up to 3072 filters rows of more than 16384 ids; those calls must not overlap in time on
  * the GPU with others that were given the same workspace. */
 size_t scd_workspace_bytes(const scd_config* cfg);
@@ -252,7 +252,7 @@ int scd_verify(scd_ctx* ctx, const uint8_t* d_k, const int32_t* d_y, const int32
 int scd_step(scd_ctx* ctx, const uint16_t* d_h, const uint16_t* d_W, void* d_state);
 
 /* Optional instrumentation for benchmarks: while both events are non-NULL,
- * scd_step and scd_step_quantized launch the LM-head kernel with the two events attached to the
+ * scd_step, scd_step_quantized and scd_step_fp8 launch the LM-head kernel with the two events attached to the
  * dispatch (hipExtLaunchKernel): ev_start takes the kernel's start time, ev_stop
  * its stop time, on the context's stream; no other packet enters the stream
  * (hipEvent_t passed as void*, owned by the caller).  NULL, NULL turns it off.
@@ -372,6 +372,75 @@ int scd_cross_entropy_backward(scd_ctx* ctx, const uint16_t* d_h, const uint16_t
  * N: gemm_kernel<.., kGradient>, gemm_kernel<.., kRows> in K parts, gemm_kernel<.., kTable or kTableTwoTerms>" (255 characters
  * hold it).  SCD_OK, or SCD_EINVAL / SCD_EUNSUPPORTED as the calls.  Host-only call. */
 int scd_cross_entropy_kernel_names(scd_ctx* ctx, int32_t rows, int32_t grad_type, char* host_buf, size_t cap);
+
+/* ---- around the model's last norm, and what it leaves of the gradients ---------------------------
+ * The norm that the hidden rows pass before the LM head, the LM head over 8-bit rows and weights, and the norm of the gradients that
+ * these calls and the caller's own leave.  Pointers to rows, gains and tables are 16-byte aligned, float arrays and scales 4-byte.  Of the
+ * configuration the norms use d (in 8 .. 2^24), the calls on gradients nothing. */
+
+/* Type of a residual stream, a gain, a tensor. */
+typedef enum scd_type {
+  SCD_BF16 = 0,
+  SCD_F32 = 1
+} scd_type;
+
+/* Root-mean-square norm with the residual's addition, rows of d:
+ *   s = x + r,  inv = 1 / sqrt(mean(s^2) + eps),  y = s * inv * gain        (in fp32; each result rounded once)
+ *   d_x bf16 [rows, d];  d_residual [rows, d] of type stream_type, or NULL (s = x);  d_gain [d] of type gain_type;  eps > 0;
+ *   d_y bf16 [rows, d];  d_sum [rows, d] of type stream_type: s (NULL: not wanted, and without a residual);  d_inv fp32 [rows], for
+ * the gradient (NULL: not wanted).  d_sum may be d_residual, d_y may be d_x; nothing else may overlap.  rows = 0 is allowed (arrays of no
+ * elements may then be NULL), up to 2^25. */
+int scd_norm(scd_ctx* ctx, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
+             int32_t rows, uint16_t* d_y, void* d_sum, float* d_inv);
+
+/* The same with y in 8 bits: d_codes e4m3 (4 exponent and 3 mantissa bits, no infinities) [rows, d] and d_scales fp32 [rows, ceil(d / 128)],
+ *   scale = max |y| / 448 over 128 of a row,  code = y / scale, rounded to the nearest.
+ * 128 values of which none reaches 448 * 2^-126 count as zeros (scale and codes 0); with an infinity among them the scale is infinite,
+ * with a NaN a NaN. */
+int scd_norm_fp8(scd_ctx* ctx, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
+                 int32_t rows, uint8_t* d_codes, float* d_scales, void* d_sum, float* d_inv);
+
+/* Gradient of both (of y as it is before its rounding) with respect to the rows and the gains:
+ *   dx = inv * (a - s * inv^2 * mean(a * s)) + ds,  a = gain * dy;   dgain = sum over the rows of dy * s * inv
+ *   d_sum (s: without a residual x, with stream_type SCD_BF16) and d_inv as scd_norm left them;  d_dy bf16 [rows, d];  d_dsum [rows, d] of
+ * type grad_type: the gradient that reaches s from elsewhere, or NULL;  d_dx [rows, d] of type grad_type: the gradient of x and of the
+ * residual alike; it may be d_dsum, or d_dy if it is bf16;  d_dgain [d] of type gain_grad_type, or NULL, added to with accumulate = 1 (in 32 bits,
+ * rounded once).  The same call gives the same bits.  The workspace is the caller's, 256-byte aligned, of the size that the query gives
+ * (0 for bad arguments); nothing in it outlives the call, and calls that may overlap in time must not share one. */
+size_t scd_norm_backward_workspace_bytes(const scd_config* cfg, int32_t rows);
+int scd_norm_backward(scd_ctx* ctx, const void* d_sum, int32_t stream_type, const void* d_gain, int32_t gain_type, const float* d_inv,
+                      const uint16_t* d_dy, const void* d_dsum, int32_t grad_type, int32_t rows, void* d_dx, void* d_dgain,
+                      int32_t gain_grad_type, int32_t accumulate, void* d_workspace, size_t workspace_bytes);
+
+/* The LM head over e4m3 rows and weights with a scale for each block of 128:
+ *   logit[m, v] = sum over the blocks b of k of  sh[m, b] * sw[v / 128, b] * sum over k in b of h[m, k] * W[v, k]
+ *   d_h e4m3 [B, C, L, d] and d_h_scales fp32 [B, C, L, G], as scd_norm_fp8 writes them;  d_W e4m3 [V, d] and d_W_scales fp32
+ * [ceil(V / 128), G], G = ceil(d / 128), as scd_quantize_fp8 writes them (blocks of 128 ids from id 0 on, the last block of a row or of the
+ * table may be smaller).  Only rows [v_lo, v_hi) of W are read.  Products are exact and added up in fp32.  d a multiple of 16 up to 2^20, at most
+ * 2^30 allowed ids (SCD_EUNSUPPORTED beyond). */
+int scd_quantize_fp8(scd_ctx* ctx, const uint16_t* d_W, uint8_t* d_codes, float* d_scales);
+int scd_lm_head_fp8(scd_ctx* ctx, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, float* d_z);
+int scd_step_fp8(scd_ctx* ctx, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, void* d_state);
+
+/* scd_lm_head_kernel_name of these two, which launch the same kernel: lm_head_fp8_kernel<Fp8Cfg<1 + CFG, blocks of 32 window rows, columns,
+ * wavefronts along the columns, along the rows, stages of h, of W>> (127 characters hold it). */
+int scd_lm_head_fp8_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
+
+/* Norm of many gradients together, sqrt(sum of all elements' squares) (added up in 64 bits, stored as fp32), and clipping,
+ *   out = g * min(1, max_norm / norm), rounded once.
+ * Arrays of `count` tensors in HOST memory, read during the call; a tensor's d is aligned to its elements, n >= 0 (up to 2^40; d may be NULL
+ * for n = 0), type a scd_type.  d_norm fp32, one element: written by scd_gradient_norm, read by scd_clip_gradients, which takes any norm that
+ * the caller puts there (of several machines' gradients together, say).  out[i] has the elements of grads[i], in either type; it may be
+ * the same tensor (of the same type: left alone where norm <= max_norm); otherwise nothing may overlap.  A norm that is infinite leaves
+ * zeros (NaN where the gradient is infinite), one that is NaN makes all NaN.  max_norm >= 0.  Workspace as in scd_norm_backward. */
+typedef struct scd_tensor {
+  void* d;
+  int64_t n;
+  int32_t type;
+} scd_tensor;
+size_t scd_gradient_norm_workspace_bytes(const scd_tensor* grads, int32_t count);
+int scd_gradient_norm(scd_ctx* ctx, const scd_tensor* grads, int32_t count, float* d_norm, void* d_workspace, size_t workspace_bytes);
+int scd_clip_gradients(scd_ctx* ctx, const scd_tensor* grads, const scd_tensor* out, int32_t count, float max_norm, const float* d_norm);
 
 /* Synchronises the stream and reports: host_flags[0] = numeric-fault bits,
  * host_flags[1] = 1 if every sequence has emitted N tokens, host_flags[2] =

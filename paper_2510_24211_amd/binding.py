@@ -46,6 +46,10 @@ class ScdQuantized(ctypes.Structure):
     _fields_ = [("d_packed", ctypes.c_void_p), ("group", ctypes.c_int32), ("zeros", ctypes.c_int32)]
 
 
+class ScdTensor(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
 class ScdError(RuntimeError):
     def __init__(self, code, what):
         super().__init__(f"{what}: {code} ({strerror(code)})")
@@ -105,6 +109,20 @@ def load():
     lib.scd_cross_entropy_backward_workspace_bytes.argtypes = [cfgp, i32, i32]
     lib.scd_cross_entropy_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, sz]
     lib.scd_cross_entropy_kernel_names.argtypes = [vp, i32, i32, ctypes.c_char_p, sz]
+    tensorp = ctypes.POINTER(ScdTensor)
+    lib.scd_norm.argtypes = [vp, vp, vp, i32, vp, i32, f32, i32, vp, vp, vp]
+    lib.scd_norm_fp8.argtypes = [vp, vp, vp, i32, vp, i32, f32, i32, vp, vp, vp, vp]
+    lib.scd_norm_backward_workspace_bytes.restype = sz
+    lib.scd_norm_backward_workspace_bytes.argtypes = [cfgp, i32]
+    lib.scd_norm_backward.argtypes = [vp, vp, i32, vp, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, sz]
+    lib.scd_quantize_fp8.argtypes = [vp, vp, vp, vp]
+    lib.scd_lm_head_fp8.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.scd_step_fp8.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.scd_lm_head_fp8_kernel_name.argtypes = [vp, ctypes.c_char_p, sz]
+    lib.scd_gradient_norm_workspace_bytes.restype = sz
+    lib.scd_gradient_norm_workspace_bytes.argtypes = [tensorp, i32]
+    lib.scd_gradient_norm.argtypes = [vp, tensorp, i32, vp, vp, sz]
+    lib.scd_clip_gradients.argtypes = [vp, tensorp, tensorp, i32, f32, vp]
     lib.scd_status.argtypes = [vp, vp, ctypes.POINTER(i32 * 4)]
     lib.scd_strerror.restype = ctypes.c_char_p
     lib.scd_strerror.argtypes = [ctypes.c_int]
@@ -115,7 +133,8 @@ def load():
                  "scd_set_lm_head_events", "scd_lm_head_kernel_name", "scd_quantize",
                  "scd_pack_quantized", "scd_lm_head_quantized", "scd_step_quantized", "scd_lm_head_quantized_kernel_name", "scd_embed", "scd_embed_window",
                  "scd_embed_backward", "scd_cross_entropy", "scd_cross_entropy_backward",
-                 "scd_cross_entropy_kernel_names", "scd_status", "scdw_gather_hidden", "scdw_copy"):
+                 "scd_cross_entropy_kernel_names", "scd_norm", "scd_norm_fp8", "scd_norm_backward", "scd_quantize_fp8",
+                 "scd_lm_head_fp8", "scd_step_fp8", "scd_lm_head_fp8_kernel_name", "scd_gradient_norm", "scd_clip_gradients", "scd_status", "scdw_gather_hidden", "scdw_copy"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -171,6 +190,36 @@ def _grad_type(dtype):
     if dtype not in _GRAD:
         raise TypeError(f"gradient of W: dtype {dtype}, expected one of {tuple(_GRAD)}")
     return _GRAD[dtype]
+
+
+_E4M3 = (torch.float8_e4m3fn, torch.uint8)
+BF16, F32 = 0, 1
+_TYPE = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _type(t, what):
+    """scd_type of a tensor; of none, any."""
+    if t is None:
+        return BF16
+    if not isinstance(t, torch.Tensor) or t.dtype not in _TYPE:
+        raise TypeError(f"{what}: expected a tensor of one of {tuple(_TYPE)}")
+    return _TYPE[t.dtype]
+
+
+class TensorList:
+    """Tensors (contiguous, bf16 or fp32, views among them) as gradient_norm and clip_gradients take them; it keeps them alive."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (ScdTensor * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            p = _ptr(t, tuple(_TYPE), 0, f"tensor {i}")
+            if p is None:
+                raise TypeError(f"tensor {i}: expected a CUDA tensor")
+            self.array[i] = ScdTensor(p.value, t.numel(), _TYPE[t.dtype])
+
+    def __len__(self):
+        return len(self.tensors)
 
 
 class QuantizedWeights:
@@ -423,6 +472,95 @@ class Scd:
         self._check(self.lib.scd_cross_entropy_kernel_names(self.ctx, _int32(rows, "rows"), _grad_type(grad_dtype), buf, 256),
                     "scd_cross_entropy_kernel_names")
         return buf.value.decode()
+
+    # -- around the last norm, and what it leaves of the gradients ----------------
+    def _rows(self, t, what):
+        if not isinstance(t, torch.Tensor) or t.numel() % max(1, self.cfg.d):
+            raise ValueError(f"{what}: expected a tensor of whole rows of {self.cfg.d}")
+        return _int32(t.numel() // max(1, self.cfg.d), what)
+
+    def _norm_stream(self, rows, residual, sum):
+        """Pointers and type of the residual stream before and behind the addition."""
+        if residual is not None and sum is not None and residual.dtype != sum.dtype:
+            raise TypeError(f"sum: dtype {sum.dtype}, the residual's is {residual.dtype}")
+        n = rows * self.cfg.d
+        return (_ptr(residual, tuple(_TYPE), n, "residual"), _type(residual, "residual"), _ptr(sum, tuple(_TYPE), n, "sum"))
+
+    def norm(self, x, gain, y, eps, residual=None, sum=None, inv=None):
+        """y = s * inv * gain, s = x + residual (kept in sum, which may be residual), inv = 1 / sqrt(mean(s^2) + eps)."""
+        rows = self._rows(x, "x")
+        r, stream, s = self._norm_stream(rows, residual, sum)
+        self._check(self.lib.scd_norm(
+            self.ctx, _ptr(x, _BF16, rows * self.cfg.d, "x"), r, stream, _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
+            float(eps), rows, _ptr(y, _BF16, rows * self.cfg.d, "y"), s, _ptr(inv, (torch.float32,), rows, "inv")), "scd_norm")
+
+    def norm_fp8(self, x, gain, codes, scales, eps, residual=None, sum=None, inv=None):
+        """The same with y as e4m3 codes and a scale per 128 of a row."""
+        rows, G = self._rows(x, "x"), -(-self.cfg.d // 128)
+        r, stream, s = self._norm_stream(rows, residual, sum)
+        self._check(self.lib.scd_norm_fp8(
+            self.ctx, _ptr(x, _BF16, rows * self.cfg.d, "x"), r, stream, _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
+            float(eps), rows, _ptr(codes, _E4M3, rows * self.cfg.d, "codes"), _ptr(scales, (torch.float32,), rows * G, "scales"), s,
+            _ptr(inv, (torch.float32,), rows, "inv")), "scd_norm_fp8")
+
+    def norm_backward_workspace(self, rows):
+        return self._workspace(self.lib.scd_norm_backward_workspace_bytes(ctypes.byref(self.cfg), _int32(rows, "rows")),
+                               "scd_norm_backward_workspace_bytes")
+
+    def norm_backward(self, sum, gain, inv, dy, dx, dgain, workspace, dsum=None, accumulate=False):
+        """dx (bf16 or fp32, as dsum): gradient of x and of the residual; dgain (bf16 or fp32, or None) = or += the gains'."""
+        rows = self._rows(sum, "sum")
+        n = rows * self.cfg.d
+        if dsum is not None and dsum.dtype != dx.dtype:
+            raise TypeError(f"dsum: dtype {dsum.dtype}, dx's is {dx.dtype}")
+        self._check(self.lib.scd_norm_backward(
+            self.ctx, _ptr(sum, tuple(_TYPE), n, "sum"), _type(sum, "sum"), _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
+            _ptr(inv, (torch.float32,), rows, "inv"), _ptr(dy, _BF16, n, "dy"), _ptr(dsum, tuple(_TYPE), n, "dsum"), _type(dx, "dx"), rows,
+            _ptr(dx, tuple(_TYPE), n, "dx"), _ptr(dgain, tuple(_TYPE), self.cfg.d, "dgain"), _type(dgain, "dgain"), int(accumulate),
+            _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()), "scd_norm_backward")
+
+    def quantize_fp8(self, W, codes, scales):
+        """W as e4m3 codes and a scale for each block of 128 x 128."""
+        c = self.cfg
+        G = -(-c.d // 128)
+        self._check(self.lib.scd_quantize_fp8(
+            self.ctx, _ptr(W, _BF16, c.V * c.d, "W"), _ptr(codes, _E4M3, c.V * c.d, "codes"),
+            _ptr(scales, (torch.float32,), -(-c.V // 128) * G, "scales")), "scd_quantize_fp8")
+
+    def _fp8(self, h, h_scales, W, W_scales):
+        c = self.cfg
+        rows, G = c.B * self.C * c.L, -(-c.d // 128)
+        return (_ptr(h, _E4M3, rows * c.d, "h"), _ptr(h_scales, (torch.float32,), rows * G, "h_scales"), _ptr(W, _E4M3, c.V * c.d, "W"),
+                _ptr(W_scales, (torch.float32,), -(-c.V // 128) * G, "W_scales"))
+
+    def lm_head_fp8(self, h, h_scales, W, W_scales, z):
+        self._check(self.lib.scd_lm_head_fp8(
+            self.ctx, *self._fp8(h, h_scales, W, W_scales), _ptr(z, (torch.float32,), self.cfg.B * self.cfg.L * self.n, "z")), "scd_lm_head_fp8")
+
+    def step_fp8(self, h, h_scales, W, W_scales, state):
+        self._check(self.lib.scd_step_fp8(
+            self.ctx, *self._fp8(h, h_scales, W, W_scales), _ptr(state, (torch.uint8,), state_bytes(self.cfg), "state")), "scd_step_fp8")
+
+    def lm_head_fp8_kernel_name(self):
+        buf = ctypes.create_string_buffer(128)
+        self._check(self.lib.scd_lm_head_fp8_kernel_name(self.ctx, buf, 128), "scd_lm_head_fp8_kernel_name")
+        return buf.value.decode()
+
+    def gradient_norm_workspace(self, grads):
+        return self._workspace(self.lib.scd_gradient_norm_workspace_bytes(grads.array, len(grads)), "scd_gradient_norm_workspace_bytes")
+
+    def gradient_norm(self, grads, norm, workspace):
+        """norm[0] = the 2-norm of all tensors of a TensorList together."""
+        self._check(self.lib.scd_gradient_norm(
+            self.ctx, grads.array, len(grads), _ptr(norm, (torch.float32,), 1, "norm"), _ptr(workspace, (torch.uint8,), 1, "workspace"),
+            workspace.numel()), "scd_gradient_norm")
+
+    def clip_gradients(self, grads, out, max_norm, norm):
+        """out[i] = grads[i] * min(1, max_norm / norm[0]); out may be grads."""
+        if len(grads) != len(out):
+            raise ValueError(f"{len(out)} outputs for {len(grads)} tensors")
+        self._check(self.lib.scd_clip_gradients(
+            self.ctx, grads.array, out.array, len(grads), float(max_norm), _ptr(norm, (torch.float32,), 1, "norm")), "scd_clip_gradients")
 
     # -- benchmark plumbing ---------------------------------------------------
     def gather_hidden(self, table, age_cap, state, h):

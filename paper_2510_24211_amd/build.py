@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libscd.so")
 SOURCES = ["scd_api.hip", "lm_head.hip", "row.hip", "row_batched.hip", "row_short.hip", "commit.hip",
            "workload_gather.hip", "lm_head_quantized.hip",
-           "embed.hip", "cross_entropy.hip"]
+           "embed.hip", "cross_entropy.hip", "lm_head_fp8.hip", "norm.hip", "clip.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          # the method's fp32 roundings are part of its definition: no fused contraction
          "-ffp-contract=off",

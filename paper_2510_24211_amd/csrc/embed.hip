@@ -15,17 +15,12 @@
 //   In sorting, every block of 2048 rows reads the digits' counts of all blocks: a term that grows with the square of the rows.  It is lost in the
 // rest up to some 2^20 rows (all of the gradient for rows of 8 columns: 186 us for 2^20 rows, 0.75 ms for 2^22) and is nearly all there is at the
 // limit of 2^25 (21 ms).
+#include "eights.h"
 #include "scd_device.h"
 #include "scd_kernels.h"
-#include "tile_loads.h"
 
 namespace scd {
 namespace {
-
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x8 widen(u32x4 v) { return __builtin_convertvector(__builtin_bit_cast(bf16x8, v), f32x8); }
-__device__ __forceinline__ u32x4 narrow(f32x8 v) { return __builtin_bit_cast(u32x4, __builtin_convertvector(v, bf16x8)); }
 
 // ---- lookup ------------------------------------------------------------------------------------
 // A wavefront per row and 512 pieces of 16 bytes; all of its loads are under way before the first store.
@@ -284,7 +279,6 @@ constexpr uint32_t kZeroIds = 16;
 template <bool F32, bool ACC>
 __device__ __forceinline__ void put(void* dW, int64_t id, int d, int col, f32x8 v) {
   if constexpr (F32) {
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
     f32x4* const to = reinterpret_cast<f32x4*>(static_cast<float*>(dW) + id * d + col);
     f32x4 a{v[0], v[1], v[2], v[3]}, b{v[4], v[5], v[6], v[7]};
     if (ACC) {

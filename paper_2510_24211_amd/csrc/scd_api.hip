@@ -395,6 +395,54 @@ int cross_entropy_args(scd_ctx* c, const uint16_t* d_h, const uint16_t* d_W, con
   return SCD_OK;
 }
 
+inline bool valid_type(int32_t type) { return type == SCD_BF16 || type == SCD_F32; }
+
+int norm_args(scd_ctx* c, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
+              int32_t rows, void* d_y, void* d_sum, float* d_inv, scd::NormArgs* a) {
+  if (!c || c->cfg.d <= 0 || c->cfg.d > kEmbedWidth || rows < 0 || rows > kEmbedRows || !d_gain || (rows > 0 && (!d_x || !d_y))) return SCD_EINVAL;
+  if (!valid_type(stream_type) || !valid_type(gain_type) || !(eps > 0.f) || !std::isfinite(eps) || (d_sum && !d_residual && rows > 0)) return SCD_EINVAL;
+  if (!aligned(d_x, 16) || !aligned(d_residual, 16) || !aligned(d_gain, 16) || !aligned(d_sum, 16) || !aligned(d_inv, 4)) return SCD_EINVAL;
+  a->x = d_x; a->residual = d_residual; a->gain = d_gain; a->y = d_y; a->sum = d_sum; a->inv = d_inv;
+  a->rows = rows; a->d = c->cfg.d; a->eps = eps;
+  a->stream_f32 = stream_type == SCD_F32; a->gain_f32 = gain_type == SCD_F32;
+  return SCD_OK;
+}
+
+int fp8_args(scd_ctx* c, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, scd::LmHeadArgs* a) {
+  if (!c || !d_h || !d_h_scales || !d_W || !d_W_scales || c->cfg.d <= 0) return SCD_EINVAL;
+  if (!aligned(d_h, 16) || !aligned(d_h_scales, 4) || !aligned(d_W, 16) || !aligned(d_W_scales, 4)) return SCD_EINVAL;
+  if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20) || c->n > kMostIds) return SCD_EUNSUPPORTED;
+  a->h = reinterpret_cast<const uint16_t*>(d_h);
+  a->B = c->cfg.B; a->C = c->C; a->L = c->cfg.L; a->N = c->cfg.N; a->d = c->cfg.d; a->n = c->n;
+  a->lam = c->cfg.cfg_lambda;
+  a->one_plus_lam = 1.0f + c->cfg.cfg_lambda;
+  a->tau = c->cfg.temperature;
+  return scd::lm_head_fp8_fits(*a) ? SCD_OK : SCD_EUNSUPPORTED;
+}
+
+// The list as the launchers take it, in host memory of its own.
+struct GradientList {
+  scd::GradientTensor* g;
+  ~GradientList() { delete[] g; }
+};
+int gradient_list(const scd_tensor* in, const scd_tensor* out, int32_t count, GradientList* list) {
+  if (count < 0 || (count > 0 && !in)) return SCD_EINVAL;
+  list->g = new (std::nothrow) scd::GradientTensor[static_cast<size_t>(count) + 1];
+  if (!list->g) return SCD_EINVAL;
+  auto valid = [](const scd_tensor& t) {
+    return t.n >= 0 && t.n <= static_cast<int64_t>(1) << 40 && valid_type(t.type) && (t.n == 0 || t.d) && aligned(t.d, t.type == SCD_F32 ? 4 : 2);
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    if (!valid(in[i])) return SCD_EINVAL;
+    list->g[i] = scd::GradientTensor{in[i].d, nullptr, in[i].n, in[i].type == SCD_F32, false};
+    if (!out) continue;
+    if (!valid(out[i]) || out[i].n != in[i].n || (in[i].n > 0 && out[i].d == in[i].d && out[i].type != in[i].type)) return SCD_EINVAL;
+    list->g[i].out = out[i].d;
+    list->g[i].out_f32 = out[i].type == SCD_F32;
+  }
+  return SCD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -654,6 +702,106 @@ int scd_cross_entropy_kernel_names(scd_ctx* c, int32_t rows, int32_t grad_type, 
   if (c->C != 1 || !cross_entropy_fits(rows, c->n, c->cfg.d, c->cfg.temperature)) return SCD_EUNSUPPORTED;
   const int len = scd::cross_entropy_kernel_names(rows, c->n, c->cfg.d, grad_type == SCD_GRAD_F32, host_buf, cap);
   return static_cast<size_t>(len) >= cap ? SCD_EINVAL : SCD_OK;
+}
+
+// ---- around the last norm ----------------------------------------------------------------
+int scd_norm(scd_ctx* c, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
+             int32_t rows, uint16_t* d_y, void* d_sum, float* d_inv) {
+  scd::NormArgs a{};
+  if (!aligned(d_y, 16)) return SCD_EINVAL;
+  if (int rc = norm_args(c, d_x, d_residual, stream_type, d_gain, gain_type, eps, rows, d_y, d_sum, d_inv, &a); rc != SCD_OK) return rc;
+  return hip_rc(scd::launch_norm(a, c->stream));
+}
+
+int scd_norm_fp8(scd_ctx* c, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
+                 int32_t rows, uint8_t* d_codes, float* d_scales, void* d_sum, float* d_inv) {
+  scd::NormArgs a{};
+  if (!aligned(d_codes, 16) || !aligned(d_scales, 4) || (rows > 0 && !d_scales)) return SCD_EINVAL;
+  if (int rc = norm_args(c, d_x, d_residual, stream_type, d_gain, gain_type, eps, rows, d_codes, d_sum, d_inv, &a); rc != SCD_OK) return rc;
+  a.scales = d_scales;
+  return hip_rc(scd::launch_norm(a, c->stream));
+}
+
+size_t scd_norm_backward_workspace_bytes(const scd_config* cfg, int32_t rows) {
+  if (!valid_config(cfg) || cfg->d <= 0 || cfg->d > kEmbedWidth || rows < 0 || rows > kEmbedRows) return 0;
+  return scd::norm_backward_bytes(rows, cfg->d);
+}
+
+int scd_norm_backward(scd_ctx* c, const void* d_sum, int32_t stream_type, const void* d_gain, int32_t gain_type, const float* d_inv,
+                      const uint16_t* d_dy, const void* d_dsum, int32_t grad_type, int32_t rows, void* d_dx, void* d_dgain,
+                      int32_t gain_grad_type, int32_t accumulate, void* d_workspace, size_t workspace_bytes) {
+  if (!c || c->cfg.d <= 0 || c->cfg.d > kEmbedWidth || rows < 0 || rows > kEmbedRows || !d_gain) return SCD_EINVAL;
+  if (rows > 0 && (!d_sum || !d_inv || !d_dy || !d_dx)) return SCD_EINVAL;
+  if (!valid_type(stream_type) || !valid_type(gain_type) || !valid_type(grad_type) || !valid_type(gain_grad_type) || (accumulate != 0 && accumulate != 1))
+    return SCD_EINVAL;
+  if (!aligned(d_sum, 16) || !aligned(d_gain, 16) || !aligned(d_inv, 4) || !aligned(d_dy, 16) || !aligned(d_dsum, 16) || !aligned(d_dx, 16) ||
+      !aligned(d_dgain, 16))
+    return SCD_EINVAL;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::norm_backward_bytes(rows, c->cfg.d))) return SCD_EWORKSPACE;
+  scd::NormBackwardArgs a{};
+  a.sum = d_sum; a.gain = d_gain; a.inv = d_inv; a.dy = d_dy; a.dsum = d_dsum; a.dx = d_dx; a.dgain = d_dgain;
+  a.rows = rows; a.d = c->cfg.d;
+  a.stream_f32 = stream_type == SCD_F32; a.gain_f32 = gain_type == SCD_F32; a.grad_f32 = grad_type == SCD_F32;
+  a.dgain_f32 = gain_grad_type == SCD_F32; a.accumulate = accumulate != 0;
+  a.ws = d_workspace;
+  return hip_rc(scd::launch_norm_backward(a, c->stream));
+}
+
+int scd_quantize_fp8(scd_ctx* c, const uint16_t* d_W, uint8_t* d_codes, float* d_scales) {
+  if (!c || !d_W || !d_codes || !d_scales || c->cfg.d <= 0 || !aligned(d_W, 16) || !aligned(d_codes, 16) || !aligned(d_scales, 4)) return SCD_EINVAL;
+  if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20)) return SCD_EUNSUPPORTED;
+  return hip_rc(scd::launch_quantize_fp8(d_W, c->cfg.V, c->cfg.d, d_codes, d_scales, c->stream));
+}
+
+int scd_lm_head_fp8(scd_ctx* c, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, float* d_z) {
+  scd::LmHeadArgs a{};
+  if (!d_z || !aligned(d_z, 4)) return SCD_EINVAL;
+  if (int rc = fp8_args(c, d_h, d_h_scales, d_W, d_W_scales, &a); rc != SCD_OK) return rc;
+  a.z = d_z;
+  return hip_rc(scd::launch_lm_head_fp8(a, d_h_scales, d_W, d_W_scales, c->cfg.v_lo, c->stream));
+}
+
+int scd_step_fp8(scd_ctx* c, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, void* st) {
+  scd::LmHeadArgs a{};
+  if (!st || !aligned(st, kAlign)) return SCD_EINVAL;
+  if (int rc = fp8_args(c, d_h, d_h_scales, d_W, d_W_scales, &a); rc != SCD_OK) return rc;
+  a.z = field<float>(c, st, SCD_F_Z);
+  a.pos = field<int32_t>(c, st, SCD_F_POS);
+  a.iter = field<int32_t>(c, st, SCD_F_ITER);
+  a.parity_stride = static_cast<size_t>(c->cfg.B) * c->cfg.L * c->n;
+  const bool timed = c->ev_start && c->ev_stop;
+  if (scd::launch_lm_head_fp8(a, d_h_scales, d_W, d_W_scales, c->cfg.v_lo, c->stream, timed ? c->ev_start : nullptr, timed ? c->ev_stop : nullptr) !=
+      hipSuccess)
+    return SCD_EHIP;
+  return run_tail(c, st, 0, nullptr);
+}
+
+int scd_lm_head_fp8_kernel_name(scd_ctx* c, char* host_buf, size_t cap) {
+  if (!c || !host_buf || c->cfg.d <= 0) return SCD_EINVAL;
+  scd::LmHeadArgs a{};
+  a.B = c->cfg.B; a.C = c->C; a.L = c->cfg.L; a.d = c->cfg.d; a.n = c->n;
+  if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20) || c->n > kMostIds || !scd::lm_head_fp8_fits(a)) return SCD_EUNSUPPORTED;
+  return static_cast<size_t>(scd::lm_head_fp8_kernel_name(a, host_buf, cap)) >= cap ? SCD_EINVAL : SCD_OK;
+}
+
+size_t scd_gradient_norm_workspace_bytes(const scd_tensor* grads, int32_t count) {
+  GradientList list{};
+  return gradient_list(grads, nullptr, count, &list) == SCD_OK ? scd::gradient_norm_bytes(list.g, count) : 0;
+}
+
+int scd_gradient_norm(scd_ctx* c, const scd_tensor* grads, int32_t count, float* d_norm, void* d_workspace, size_t workspace_bytes) {
+  if (!c || !d_norm || !aligned(d_norm, 4)) return SCD_EINVAL;
+  GradientList list{};
+  if (int rc = gradient_list(grads, nullptr, count, &list); rc != SCD_OK) return rc;
+  if (!valid_workspace(d_workspace, workspace_bytes, scd::gradient_norm_bytes(list.g, count))) return SCD_EWORKSPACE;
+  return hip_rc(scd::launch_gradient_norm(list.g, count, d_norm, d_workspace, c->stream));
+}
+
+int scd_clip_gradients(scd_ctx* c, const scd_tensor* grads, const scd_tensor* out, int32_t count, float max_norm, const float* d_norm) {
+  if (!c || !d_norm || !aligned(d_norm, 4) || !(max_norm >= 0.f) || (count > 0 && !out)) return SCD_EINVAL;
+  GradientList list{};
+  if (int rc = gradient_list(grads, out, count, &list); rc != SCD_OK) return rc;
+  return hip_rc(scd::launch_clip_gradients(list.g, count, max_norm, d_norm, c->stream));
 }
 
 int scd_status(scd_ctx* c, void* st, int32_t host_flags[4]) {

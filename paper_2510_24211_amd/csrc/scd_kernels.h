@@ -234,4 +234,56 @@ hipError_t launch_lm_head_quantized(const LmHeadArgs& a, const void* packed, int
 // Name of the kernel that it picks (B, C, L, d and n are read); snprintf semantics.
 int lm_head_quantized_kernel_name(const LmHeadArgs& a, int group, bool zeros, char* buf, size_t cap);
 
+// The LM head over e4m3 rows [B, C, L, d] (LmHeadArgs::h, 16-byte aligned) and an e4m3 table [V, d], with a scale for each 128 of a row of h
+// and for each 128 x 128 of the table.
+hipError_t launch_quantize_fp8(const uint16_t* W, int V, int d, uint8_t* codes, float* scales, hipStream_t s);
+hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const uint8_t* W, const float* W_scales, int v_lo, hipStream_t s,
+                              hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);      // as in launch_lm_head
+// whether its launch can hold the tiles of a call of these sizes (B, C, L, n are read)
+bool lm_head_fp8_fits(const LmHeadArgs& a);
+// Name of the kernel that it picks (B, C, L, d and n are read); snprintf semantics.
+int lm_head_fp8_kernel_name(const LmHeadArgs& a, char* buf, size_t cap);
+
+// ---- norm of hidden rows -------------------------------------------------------------
+struct NormArgs {
+  const uint16_t* x;         // bf16 [rows, d]
+  const void* residual;      // [rows, d] of the stream's type, or null
+  const void* gain;          // [d], bf16 or fp32
+  void* y;                   // [rows, d]: bf16, or e4m3 codes where there are scales
+  float* scales;             // [rows, ceil(d / 128)] or null
+  void* sum;                 // [rows, d] of the stream's type, or null
+  float* inv;                // [rows] or null
+  int rows, d;
+  float eps;
+  bool stream_f32, gain_f32;
+};
+hipError_t launch_norm(const NormArgs& a, hipStream_t s);
+
+struct NormBackwardArgs {
+  const void* sum;           // [rows, d] of the stream's type
+  const void* gain;          // [d]
+  const float* inv;          // [rows]
+  const uint16_t* dy;        // bf16 [rows, d]
+  const void* dsum;          // [rows, d] of dx's type, or null
+  void* dx;                  // [rows, d], bf16 or fp32
+  void* dgain;               // [d], bf16 or fp32, or null
+  int rows, d;
+  bool stream_f32, gain_f32, grad_f32, dgain_f32, accumulate;
+  void* ws;                  // norm_backward_bytes(rows, d), 256-byte aligned
+  float *part, *mean;        // set by launch_norm_backward
+};
+size_t norm_backward_bytes(int rows, int d);
+hipError_t launch_norm_backward(const NormBackwardArgs& a, hipStream_t s);
+
+// ---- norm of many gradients, and clipping -----------------------------------------------
+struct GradientTensor {
+  const void* in;
+  void* out;                 // clipping
+  int64_t n;
+  bool in_f32, out_f32;
+};
+size_t gradient_norm_bytes(const GradientTensor* g, int count);
+hipError_t launch_gradient_norm(const GradientTensor* g, int count, float* norm, void* ws, hipStream_t s);
+hipError_t launch_clip_gradients(const GradientTensor* g, int count, float most, const float* norm, hipStream_t s);
+
 }  // namespace scd
