@@ -8,8 +8,8 @@
 // exactly, products are exact and sums keep fp32's bits (1e-8 to 7e-8 there).  So codes stay 8 bits wide in memory and LDS and are
 // converted, two by an instruction, on their way from LDS to the MFMAs.
 //
-// Rows of h are the MFMA's columns: a lane has one row, and one scale.  Tiles of columns begin at multiples of 128 of the table, whatever
-// the first allowed id, so that a wavefront's columns share theirs.  h, W and the scales go from memory straight into LDS, 128 bytes of a
+// Rows of h are the MFMA's columns: a lane has one row, and one scale of it; its columns' scale is one number, or two where a group of the
+// table ends among them.  h, W and the scales go from memory straight into LDS, 128 bytes of a
 // row to a stage; slot l % 8 of row l / 8 of a load holds chunk (l % 8) ^ ((row >> 1) & 7): operand reads are then free of bank conflicts.
 #include "eights.h"
 #include "launch_events.h"
@@ -29,12 +29,15 @@ __device__ __forceinline__ f16x8 to_f16(uint32_t a, uint32_t b) {
   return f16x8{v[0].x, v[0].y, v[1].x, v[1].y, v[2].x, v[2].y, v[3].x, v[3].y};
 }
 
-// RB blocks of 32 window rows (times C with guidance) x BN columns by WCOL x WROW wavefronts; SA stages of h and the scales, SB of W
-template <int C_, int RB_, int BN_, int WCOL_, int WROW_, int SA_, int SB_>
+// RB blocks of 32 window rows (times C with guidance) x BN columns by WCOL x WROW wavefronts; S stages
+// NT: W past the caches
+template <int C_, int RB_, int BN_, int WCOL_, int WROW_, int S_, bool NT_ = false>
 struct Fp8Cfg {
-  static constexpr int C = C_, RB = RB_, BN = BN_, WCOL = WCOL_, WROW = WROW_, SA = SA_, SB = SB_;
-  static int name(char* buf, size_t cap) {
-    return snprintf(buf, cap, "lm_head_fp8_kernel<Fp8Cfg<%d, %d, %d, %d, %d, %d, %d>>", C, RB, BN, WCOL, WROW, SA, SB);
+  static constexpr int C = C_, RB = RB_, BN = BN_, WCOL = WCOL_, WROW = WROW_, S = S_;
+  static constexpr bool NT = NT_;
+  static int name(char* buf, size_t cap, bool borders) {
+    return snprintf(buf, cap, "lm_head_fp8_kernel<Fp8Cfg<%d, %d, %d, %d, %d, %d, %s>, %s>", C, RB, BN, WCOL, WROW, S, NT ? "true" : "false",
+                    borders ? "true" : "false");
   }
   static constexpr int NW = WCOL * WROW, THREADS = NW * 64;
   static constexpr int HR = RB * C * 32;                   // rows of h
@@ -42,10 +45,10 @@ struct Fp8Cfg {
   static constexpr int RBW = RB / WROW, NB = RBW * C;      // blocks of rows per wavefront
   static constexpr int AL = HR / 8 / NW, BL = BN / 8 / NW; // loads per wavefront and block of k
   static constexpr int AB = HR * 128, BB = BN * 128, SCB = NW * 256;     // bytes of a stage: h, W, scales
-  static constexpr int LDS = SA * (AB + SCB) + SB * BB;
-  static_assert(CW % 32 == 0 && CW <= 128 && 128 % CW == 0 && RBW * WROW == RB && AL * NW * 8 == HR && BL * NW * 8 == BN, "tile shape");
-  static_assert(LDS <= 160 * 1024 && NW * 64 >= HR + (BN + 127) / 128 && SB >= SA && SA >= 2, "LDS");
-  static_assert((SA - 2) * (AL + BL + 1) + BL <= 63, "loads in flight");
+  static constexpr int LDS = S * (AB + BB + SCB);
+  static constexpr int ALL = AL + BL + 1;
+  static_assert((CW == 32 || CW == 64) && RBW * WROW == RB && AL * NW * 8 == HR && BL * NW * 8 == BN, "tile shape");
+  static_assert(LDS <= 160 * 1024 && NW * 64 >= HR + BN / 128 + 2 && S >= 2 && (S - 1) * ALL <= 63, "LDS, loads in flight");
 };
 
 struct Fp8Args {
@@ -64,9 +67,10 @@ __device__ __forceinline__ void load_lds4(uint64_t from, uint32_t lds) {
 }
 #pragma clang diagnostic pop
 
-template <class K>
-__global__ __launch_bounds__(K::THREADS) void lm_head_fp8_kernel(const Fp8Args f, const int WT, const int MT) {
-  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, AL = K::AL, BL = K::BL, SA = K::SA, SB = K::SB;
+// BORDERS: groups of the table may end among a wavefront's columns
+template <class K, bool BORDERS>
+__global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void lm_head_fp8_kernel(const Fp8Args f, const int WT, const int MT) {
+  constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, AL = K::AL, BL = K::BL, S = K::S;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[K::LDS];      // W's stages, then h's, then the scales'
   const LmHeadArgs& a = f.lm;
   // workgroups that share columns get ids 8 apart: the same XCD, the same L2
@@ -78,17 +82,19 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_fp8_kernel(const Fp8Args f
   const int rows = a.B * a.L, d = a.d, KT = (d + 127) / 128, G = KT;
   const int nch = d % 128 / 16;                          // 16-byte chunks of a ragged last block, 0: there is none
   const int p_base = mt * RB * 32;
-  const int col_base = (f.v_lo / 128) * 128 - f.v_lo + wt * K::BN;       // columns are counted from the first allowed id
+  const int col_base = wt * K::BN;                       // columns are counted from the first allowed id
   RowState mine[K::RBW];
 #pragma unroll
   for (int i = 0; i < K::RBW; ++i) mine[i] = row_state(a, p_base + (wr * K::RBW + i) * 32 + ln);
 
   // ---- where this lane's loads come from ----------------------------------------------------------------
   auto piece_row = [&](int per_wave, int i) { return (wave * per_wave + i) * 8 + (lane >> 3); };
-  auto piece_chunk = [&](int r) { return (lane & 7) ^ ((r >> 1) & 7); };
+  // (the rows of an even and of an odd piece: two chunks for all of a wavefront's loads)
+  auto piece_chunk = [&](int odd) { return (lane & 7) ^ ((odd * 4 + (lane >> 4)) & 7); };
+  auto odd_piece = [&](int per_wave, int i) { return per_wave % 2 == 0 ? i & 1 : (wave * per_wave + i) & 1; };
   const int h0 = first_h_row(p_base, C, a.L);
   const uint64_t hbase = reinterpret_cast<uint64_t>(a.h) + static_cast<uint64_t>(h0) * d;
-  const int w0 = max(f.v_lo + col_base, f.v_lo), w_last = f.v_lo + a.n - 1;       // first and last row of W that may be read
+  const int w0 = f.v_lo + col_base, w_last = f.v_lo + a.n - 1;       // first row of W, and the last one that may be read
   const uint64_t wbase = reinterpret_cast<uint64_t>(f.W) + static_cast<uint64_t>(w0) * d;
   auto row_of_h = [&](int r) {                           // of row r of the tile: [RB][C][32]
     const int blk = r / 32, rb = blk / C;
@@ -98,112 +104,185 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_fp8_kernel(const Fp8Args f
 #pragma unroll
   for (int i = 0; i < AL; ++i) {
     const int r = piece_row(AL, i);
-    ao[i] = static_cast<uint32_t>(row_of_h(r) - h0) * static_cast<uint32_t>(d) + piece_chunk(r) * 16;
+    ao[i] = static_cast<uint32_t>(row_of_h(r) - h0) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(AL, i)) * 16;
   }
 #pragma unroll
   for (int i = 0; i < BL; ++i) {
     const int r = piece_row(BL, i);
-    const int v = min(max(f.v_lo + col_base + r, w0), w_last);
-    bo[i] = static_cast<uint32_t>(v - w0) * static_cast<uint32_t>(d) + piece_chunk(r) * 16;
+    bo[i] = static_cast<uint32_t>(min(w0 + r, w_last) - w0) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(BL, i)) * 16;
   }
   // a word per thread: the scales of h's rows, then those of the columns' groups of 128
   uint64_t so;
   if (tid < K::HR) so = reinterpret_cast<uint64_t>(f.h_scales) + static_cast<uint64_t>(row_of_h(tid)) * G * 4;
   else {
-    const int group = (f.v_lo + col_base) / 128 + min(tid - K::HR, (K::BN - 1) / 128);
+    const int group = w0 / 128 + min(tid - K::HR, K::BN / 128 + 1);
     so = reinterpret_cast<uint64_t>(f.W_scales) + static_cast<uint64_t>(min(group, w_last / 128)) * G * 4;
   }
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds));
-  const uint32_t ldsB = lds0 + wave * BL * 1024, ldsA = lds0 + SB * K::BB + wave * AL * 1024,
-                 ldsS = lds0 + SB * K::BB + SA * K::AB + wave * 256;
+  const uint32_t ldsB = lds0 + wave * BL * 1024, ldsA = lds0 + S * K::BB + wave * AL * 1024, ldsS = lds0 + S * (K::BB + K::AB) + wave * 256;
 
-  auto back = [&](int t, int r) { return t == KT - 1 && nch != 0 ? max(piece_chunk(r) - (nch - 1), 0) * 16 : 0; };   // past a ragged end: its last chunk
-  auto load_a = [&](int t) {
-    const uint64_t at = hbase + static_cast<uint64_t>(t) * 128;
-    const uint32_t to = ldsA + t % SA * K::AB;
-    static_for<AL>([&](auto i) { load_lds16<false, decltype(i)::value * 1024>(at, ao[decltype(i)::value] - back(t, piece_row(AL, decltype(i)::value)), to); });
-    load_lds4(so + static_cast<uint64_t>(t) * 4, ldsS + t % SA * K::SCB);
+  // Blocks are walked cyclically, from one that depends on the workgroup: rows are d bytes apart, and workgroups that all begin at block 0
+  // ask the same few channels of the L2 for theirs.
+  const int rot = (MT > 1 ? id % 8 : wt) * 5 % KT;
+  auto after = [&](int k) { return k + 1 == KT ? 0 : k + 1; };
+  // Past a ragged end a row's last chunk is read: offsets of the loads of block KT - 1, made before them and taken back behind.
+  auto ragged_end = [&](int t, bool back) __attribute__((always_inline)) {
+    if (t != KT - 1 || nch == 0) return;
+    auto past = [&](int odd) { return static_cast<uint32_t>(max(piece_chunk(odd) - (nch - 1), 0) * 16); };
+#pragma unroll
+    for (int i = 0; i < AL; ++i) ao[i] += back ? past(odd_piece(AL, i)) : 0u - past(odd_piece(AL, i));
+#pragma unroll
+    for (int i = 0; i < BL; ++i) bo[i] += back ? past(odd_piece(BL, i)) : 0u - past(odd_piece(BL, i));
   };
-  auto load_b = [&](int t) {
-    const uint64_t at = wbase + static_cast<uint64_t>(t) * 128;
-    const uint32_t to = ldsB + t % SB * K::BB;
-    static_for<BL>([&](auto i) { load_lds16<false, decltype(i)::value * 1024>(at, bo[decltype(i)::value] - back(t, piece_row(BL, decltype(i)::value)), to); });
+  // Load q of block t.
+  auto load = [&](auto qq, int t, uint32_t stage) {
+    constexpr int Q = decltype(qq)::value;
+    if constexpr (Q < AL + BL) {
+      constexpr bool H = Q < AL;
+      constexpr int I = H ? Q : Q - AL;
+      load_lds16<!H && K::NT, I * 1024>((H ? hbase : wbase) + static_cast<uint64_t>(t) * 128, H ? ao[H ? I : 0] : bo[H ? 0 : I],
+                                  H ? ldsA + stage * K::AB : ldsB + stage * K::BB);
+    } else {
+      load_lds4(so + static_cast<uint64_t>(t) * 4, ldsS + stage * K::SCB);
+    }
+  };
+  // What a ragged last block lacks counts as 0: in h, by the wavefront that has loaded it.
+  auto clear_end = [&](int t, uint32_t stage) {
+    if (t != KT - 1 || nch == 0) return;
+#pragma unroll
+    for (int i = 0; i < AL; ++i)
+      if (piece_chunk(odd_piece(AL, i)) >= nch)
+        *reinterpret_cast<u32x4*>(lds + S * K::BB + stage * K::AB + (wave * AL + i) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
   };
 
-  f32x16 total[NC][NB];
+  const unsigned char* const Bt = lds + (wc * K::CW + ln) * 128;
+  const unsigned char* const At = lds + S * K::BB + (wr * NB * 32 + ln) * 128;
+  const float* const St = reinterpret_cast<const float*>(lds + S * K::BB + S * K::AB);
+  u32x4 raw[2][NB + NC];                                  // codes of two chunks: NB blocks of rows, then NC of columns
+  f16x8 op[2][NB + NC];                                   // operands of two MFMA steps
+  f32x16 total[NC][NB], acc[NC][NB];
+  // The wavefront's columns lie in one group of 128 of the table, or in two: those from `border` on have the second scale.
+  const int first = w0 + wc * K::CW, border = 128 - first % 128;
+  float scale[NB], scale2[NB], sw = 0.f, sw2 = 0.f;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int i = 0; i < NB; ++i) total[c][i] = f32x16{};
 
-  // Window t of the loads ends at the barrier of block t; it brings h of block t + SA - 1 and W of t + SB - 1 (a stage is free once the
-  // barrier behind the block that it held is passed).
-  static_for<SB - 1>([&](auto t) {
+  auto fetch = [&](auto qq, uint32_t stage) {             // chunks 2 q and 2 q + 1: 16 k for each half of the wavefront
+    constexpr int Q = decltype(qq)::value;
+    const int slot = ((Q * 2 + lg) ^ ((ln >> 1) & 7)) * 16;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) raw[Q & 1][i] = *reinterpret_cast<const u32x4*>(At + stage * K::AB + i * 4096 + slot);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) raw[Q & 1][NB + c] = *reinterpret_cast<const u32x4*>(Bt + stage * K::BB + c * 4096 + slot);
+  };
+  auto convert = [&](auto step, auto from, auto to) {     // operands [from, to) of a step (of 8 in a block)
+    constexpr int Q = decltype(step)::value / 2, E = decltype(step)::value % 2;
+#pragma unroll
+    for (int f = decltype(from)::value; f < decltype(to)::value; ++f) op[E][f] = to_f16(raw[Q & 1][f][2 * E], raw[Q & 1][f][2 * E + 1]);
+  };
+  auto add_up = [&](int c, int i) __attribute__((always_inline)) {       // the last block's sums, under its scale
+    if (BORDERS && border > c * 32 && border < c * 32 + 32) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        total[c][i][e] = __fmaf_rn(acc[c][i][e], c * 32 + e / 4 * 8 + lg * 4 + e % 4 < border ? scale[i] : scale2[i], total[c][i][e]);
+    } else {
+      const float s = !BORDERS || border > c * 32 ? scale[i] : scale2[i];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) total[c][i][e] = __fmaf_rn(acc[c][i][e], s, total[c][i][e]);
+    }
+  };
+
+  // Eight steps of 16 k make a block.  Between a step's MFMAs the next step's operands are converted, in a block's first step the sums of
+  // the block before are added up, and behind the barrier the loads of a later block are issued, one or two at a time.  Every other step begins
+  // with the reads of the next two steps' codes, which are converted behind its last MFMAs.  The barrier stands before the last step: all
+  // codes of this block are in registers then, the next block has to be in LDS, and this block's stage is free.
+  // (steps 1 to 7 of block t and step 0 of the next one: what a loop carries along is the MFMAs' own then)
+  auto step = [&](auto which, int t, int coming, int loaded, uint32_t stage, uint32_t next, auto begins, auto last) {
+    constexpr bool FIRST = decltype(begins)::value, LAST = decltype(last)::value;
+      constexpr int X = decltype(which)::value, Q = X / 2, E = X % 2;
+      if constexpr (X == 6 && !LAST) {
+        hard_fence();
+        if (t + S - 1 < KT) wait_loads<(S - 2) * K::ALL>();      // blocks t + 2 .. t + S - 1 may be on their way
+        else wait_loads<0>();
+        clear_end(coming, next);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        hard_fence();
+      }
+      if constexpr (E == 0 && !(LAST && Q == 3)) fetch(IntT<(Q + 1) % 4>{}, Q == 3 ? next : stage);
+      if constexpr (X == 4) {
+        const float* const at = St + stage * (K::SCB / 4) + K::HR + (first / 128 - w0 / 128);
+        sw = at[0];
+        if (BORDERS) sw2 = at[1];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) scale[i] = St[stage * (K::SCB / 4) + (wr * NB + i) * 32 + ln];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      constexpr int NM = NC * NB, NF = NB + NC;
+      if constexpr (X == 6 && !LAST) ragged_end(loaded, false);
+      static_for<NM>([&](auto mm) {
+        constexpr int M = decltype(mm)::value, c = M / NB, i = M % NB;
+        if constexpr (X == 0 && !FIRST) add_up(c, i);
+        acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[E][NB + c], op[E][i], X == 0 ? f32x16{} : acc[c][i], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (X >= 6 && !LAST) {
+          constexpr int SLOT = (X - 6) * NM + M, FROM = K::ALL * SLOT / (2 * NM), TO = K::ALL * (SLOT + 1) / (2 * NM);
+          if (TO > FROM && t + S < KT) static_for<TO - FROM>([&](auto j) { load(IntT<FROM + decltype(j)::value>{}, loaded, stage); });
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        constexpr int FROM = NF * M / NM, TO = NF * (M + 1) / NM;
+        if constexpr (TO > FROM && !(LAST && X == 7)) convert(IntT<(X + 1) % 8>{}, IntT<FROM>{}, IntT<TO>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (X == 7) {
+        if constexpr (!LAST) ragged_end(loaded, true);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          if (BORDERS) scale2[i] = scale[i] * sw2;
+          scale[i] *= sw;
+        }
+      }
+  };
+  auto block = [&](int t, int coming, int loaded, uint32_t stage, uint32_t next, auto last) {
+    static_for<7>([&](auto x) { step(IntT<decltype(x)::value + 1>{}, t, coming, loaded, stage, next, FalseT{}, last); });
+    if constexpr (!decltype(last)::value) step(IntT<0>{}, t + 1, coming, loaded, next, next, FalseT{}, FalseT{});
+  };
+
+  int loaded = rot, coming = after(rot);                  // blocks to be loaded next, and to be multiplied next but one
+  static_for<S>([&](auto t) {
     constexpr int T = decltype(t)::value;
-    if constexpr (T < SA - 1) {
-      if (T < KT) load_a(T);
+    if (T < KT) {
+      ragged_end(loaded, false);
+      static_for<K::ALL>([&](auto q) { load(q, loaded, T); });
+      ragged_end(loaded, true);
+      loaded = after(loaded);
     }
-    if (T < KT) load_b(T);
   });
-  // At the barrier of block t its h and W have to be there; what was issued behind h of block t may be in flight.
-  constexpr int ALL = AL + BL + 1, AHEAD = (SA - 2) * ALL + (SB > SA ? BL : 0);
-  auto multiply = [&](int t, auto ragged) {
-    constexpr bool RAGGED = decltype(ragged)::value;
-    const unsigned char* const Bt = lds + t % SB * K::BB + (wc * K::CW + ln) * 128;
-    const unsigned char* const At = lds + SB * K::BB + t % SA * K::AB + (wr * NB * 32 + ln) * 128;
-    const float* const St = reinterpret_cast<const float*>(lds + SB * K::BB + SA * K::AB + t % SA * K::SCB);
-    const float sw = St[K::HR + wc * K::CW / 128];
-    f32x16 acc[NC][NB];
-    static_for<4>([&](auto qq) {
-      constexpr int Q = decltype(qq)::value;               // chunks 2 Q and 2 Q + 1 of the block: 16 k for each half of the wavefront
-      const int chunk = Q * 2 + lg, slot = (chunk ^ ((ln >> 1) & 7)) * 16;
-      u32x4 w[NC], h[NB];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        h[i] = *reinterpret_cast<const u32x4*>(At + i * 4096 + slot);
-        if (RAGGED && chunk >= nch) h[i] = u32x4{0u, 0u, 0u, 0u};
-      }
-#pragma unroll
-      for (int c = 0; c < NC; ++c) w[c] = *reinterpret_cast<const u32x4*>(Bt + c * 4096 + slot);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        f16x8 hf[NB], wf[NC];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) hf[i] = to_f16(h[i][2 * e], h[i][2 * e + 1]);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) wf[c] = to_f16(w[c][2 * e], w[c][2 * e + 1]);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < NB; ++i)
-            acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wf[c], hf[i], Q == 0 && e == 0 ? f32x16{} : acc[c][i], 0, 0, 0);
-      }
-    });
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const float s = St[(wr * NB + i) * 32 + ln] * sw;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) total[c][i][e] = __fmaf_rn(acc[c][i][e], s, total[c][i][e]);
-    }
-  };
-  auto step = [&](int t, auto ragged) {
-    if (t + SB - 2 < KT) wait_loads<AHEAD>();            // the windows before brought all that they can
-    else wait_loads<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the last block's operands are in registers
-    __builtin_amdgcn_s_barrier();
-    hard_fence();
-    if (t + SA - 1 < KT) load_a(t + SA - 1);
-    if (t + SB - 1 < KT) load_b(t + SB - 1);
-    hard_fence();
-    multiply(t, ragged);
-    hard_fence();
-  };
-  const int full = nch != 0 ? KT - 1 : KT;
+  if (KT >= S) wait_loads<(S - 1) * K::ALL>();
+  else wait_loads<0>();
+  clear_end(rot, 0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  hard_fence();
+  fetch(IntT<0>{}, 0);
+  convert(IntT<0>{}, IntT<0>{}, IntT<NB + NC>{});
+  step(IntT<0>{}, 0, 0, 0, 0, 0, TrueT{}, FalseT{});
+  uint32_t stage = 0;
 #pragma unroll 1
-  for (int t = 0; t < full; ++t) step(t, FalseT{});
-  if (nch != 0) step(KT - 1, TrueT{});
+  for (int t = 0; t < KT - 1; ++t) {
+    const uint32_t next = stage + 1 == S ? 0 : stage + 1;
+    block(t, coming, loaded, stage, next, FalseT{});
+    stage = next;
+    coming = after(coming);
+    loaded = after(loaded);
+  }
+  block(KT - 1, 0, 0, stage, stage, TrueT{});
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) add_up(c, i);
 
   // ---- logits: a lane has a window row, a register a column --------------------------------------------------
 #pragma unroll
@@ -220,11 +299,11 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_fp8_kernel(const Fp8Args f
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           z[e] = processed_logit<C>(a, total[c][i * C][q * 4 + e], total[c][i * C + C - 1][q * 4 + e]);
-        if (col >= 0 && col + 3 < a.n) store4(row + col, z[0], z[1], z[2], z[3]);
+        if (col + 3 < a.n) store4(row + col, z[0], z[1], z[2], z[3]);
         else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (col + e >= 0 && col + e < a.n) row[col + e] = z[e];
+            if (col + e < a.n) row[col + e] = z[e];
         }
       }
   }
@@ -233,20 +312,36 @@ __global__ __launch_bounds__(K::THREADS) void lm_head_fp8_kernel(const Fp8Args f
 // ---- the shape of workgroups for a call -------------------------------------------------------------------------
 template <class K, class F>
 void with(F&& go) { go(K{}); }
+template <class K>
+int64_t tiles_of(const LmHeadArgs& a) {
+  return ((static_cast<int64_t>(a.n) + K::BN - 1) / K::BN) * ((static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32));
+}
 
+template <int C, class F>
+void choose_of(const LmHeadArgs& a, F&& go) {
+  using Large = Fp8Cfg<C, 8 / C, 128, 2, 4, 3>;            // one workgroup on a compute unit
+  using Medium = Fp8Cfg<C, 4 / C, 128, 2, 2, 2>;           // two
+  using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;              // two
+  using FewDeep = Fp8Cfg<C, 2 / C, 64, 2, 1, 6>;           // one
+  const int64_t rows = static_cast<int64_t>(a.B) * a.L * C;
+  // W is read once, and larger than what the last cache keeps from one call to the next
+  const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
+  if (rows > 128) {
+    const int64_t large = (tiles_of<Large>(a) + 255) / 256, medium = (tiles_of<Medium>(a) + 511) / 512;
+    large <= medium ? with<Large>(go) : with<Medium>(go);
+  } else if (rows > 64) {
+    past ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, true>>(go) : with<Medium>(go);
+  } else if (rows > 32 || C == 2) {
+    if (tiles_of<FewDeep>(a) <= 256) with<FewDeep>(go);
+    else past ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, true>>(go) : with<Few>(go);
+  } else if constexpr (C == 1) {
+    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 8>>(a) <= 256) with<Fp8Cfg<1, 1, 64, 2, 1, 8>>(go);
+    else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
+  }
+}
 template <class F>
 void choose(const LmHeadArgs& a, F&& go) {
-  const int64_t rows = static_cast<int64_t>(a.B) * a.L;
-  if (a.C == 2) {
-    if (rows > 64) with<Fp8Cfg<2, 4, 128, 2, 4, 3, 3>>(go);
-    else if (rows > 32) with<Fp8Cfg<2, 2, 128, 4, 1, 3, 4>>(go);
-    else with<Fp8Cfg<2, 1, 128, 4, 1, 3, 3>>(go);
-  } else {
-    if (rows > 128) with<Fp8Cfg<1, 8, 128, 2, 4, 3, 3>>(go);
-    else if (rows > 64) with<Fp8Cfg<1, 4, 128, 4, 1, 3, 4>>(go);
-    else if (rows > 32) with<Fp8Cfg<1, 2, 128, 4, 1, 3, 3>>(go);
-    else with<Fp8Cfg<1, 1, 64, 2, 1, 4, 4>>(go);
-  }
+  a.C == 2 ? choose_of<2>(a, go) : choose_of<1>(a, go);
 }
 
 // ---- weights in 8 bits ---------------------------------------------------------------------------------------------
@@ -286,8 +381,8 @@ struct Grid {
   int64_t WT, MT, groups;
 };
 template <class K>
-Grid grid_of(const LmHeadArgs& a, int v_lo) {
-  const int64_t WT = (v_lo % 128 + static_cast<int64_t>(a.n) + K::BN - 1) / K::BN, MT = (static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32);
+Grid grid_of(const LmHeadArgs& a) {
+  const int64_t WT = (static_cast<int64_t>(a.n) + K::BN - 1) / K::BN, MT = (static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32);
   return {WT, MT, (WT + 7) / 8 * 8 * MT};
 }
 }  // namespace
@@ -296,7 +391,7 @@ bool lm_head_fp8_fits(const LmHeadArgs& a) {
   bool fits = false;
   choose(a, [&](auto k) {
     using K = decltype(k);
-    fits = grid_of<K>(a, 127).groups * K::THREADS < static_cast<int64_t>(1) << 32;      // a launch's threads
+    fits = grid_of<K>(a).groups * K::THREADS < static_cast<int64_t>(1) << 32;      // a launch's threads
   });
   return fits;
 }
@@ -307,15 +402,16 @@ hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const 
   const Fp8Args f{a, h_scales, W, W_scales, v_lo};
   choose(a, [&](auto k) {
     using K = decltype(k);
-    const Grid g = grid_of<K>(a, v_lo);
-    launch_kernel(lm_head_fp8_kernel<K>, dim3(static_cast<unsigned>(g.groups)), dim3(K::THREADS), s, ev, f, static_cast<int>(g.WT), static_cast<int>(g.MT));
+    const Grid g = grid_of<K>(a);
+    launch_kernel(v_lo % 64 != 0 ? lm_head_fp8_kernel<K, true> : lm_head_fp8_kernel<K, false>, dim3(static_cast<unsigned>(g.groups)),
+                  dim3(K::THREADS), s, ev, f, static_cast<int>(g.WT), static_cast<int>(g.MT));
   });
   return hipGetLastError();
 }
 
-int lm_head_fp8_kernel_name(const LmHeadArgs& a, char* buf, size_t cap) {
+int lm_head_fp8_kernel_name(const LmHeadArgs& a, int v_lo, char* buf, size_t cap) {
   int len = 0;
-  choose(a, [&](auto k) { len = decltype(k)::name(buf, cap); });
+  choose(a, [&](auto k) { len = decltype(k)::name(buf, cap, v_lo % 64 != 0); });
   return len;
 }
 

@@ -781,7 +781,7 @@ int scd_lm_head_fp8_kernel_name(scd_ctx* c, char* host_buf, size_t cap) {
   scd::LmHeadArgs a{};
   a.B = c->cfg.B; a.C = c->C; a.L = c->cfg.L; a.d = c->cfg.d; a.n = c->n;
   if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20) || c->n > kMostIds || !scd::lm_head_fp8_fits(a)) return SCD_EUNSUPPORTED;
-  return static_cast<size_t>(scd::lm_head_fp8_kernel_name(a, host_buf, cap)) >= cap ? SCD_EINVAL : SCD_OK;
+  return static_cast<size_t>(scd::lm_head_fp8_kernel_name(a, c->cfg.v_lo, host_buf, cap)) >= cap ? SCD_EINVAL : SCD_OK;
 }
 
 size_t scd_gradient_norm_workspace_bytes(const scd_tensor* grads, int32_t count) {

@@ -242,7 +242,7 @@ hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const 
 // whether its launch can hold the tiles of a call of these sizes (B, C, L, n are read)
 bool lm_head_fp8_fits(const LmHeadArgs& a);
 // Name of the kernel that it picks (B, C, L, d and n are read); snprintf semantics.
-int lm_head_fp8_kernel_name(const LmHeadArgs& a, char* buf, size_t cap);
+int lm_head_fp8_kernel_name(const LmHeadArgs& a, int v_lo, char* buf, size_t cap);
 
 // ---- norm of hidden rows -------------------------------------------------------------
 struct NormArgs {
