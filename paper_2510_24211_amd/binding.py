@@ -159,7 +159,7 @@ def state_bytes(cfg):
 
 
 def _ptr(t, dtypes, numel, what):
-    """Device pointer of a contiguous CUDA tensor after checking dtype and size."""
+    """Device address of a contiguous CUDA tensor after checking dtype and size."""
     if t is None:
         return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -170,7 +170,7 @@ def _ptr(t, dtypes, numel, what):
         raise ValueError(f"{what}: tensor must be contiguous")
     if t.numel() < numel:
         raise ValueError(f"{what}: {t.numel()} elements, need {numel}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _int32(value, what):
@@ -216,7 +216,7 @@ class TensorList:
             p = _ptr(t, tuple(_TYPE), 0, f"tensor {i}")
             if p is None:
                 raise TypeError(f"tensor {i}: expected a CUDA tensor")
-            self.array[i] = ScdTensor(p.value, t.numel(), _TYPE[t.dtype])
+            self.array[i] = ScdTensor(p, t.numel(), _TYPE[t.dtype])
 
     def __len__(self):
         return len(self.tensors)

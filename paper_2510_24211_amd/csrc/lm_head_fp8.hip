@@ -44,11 +44,13 @@ struct Fp8Cfg {
   static constexpr int CW = BN / WCOL, NC = CW / 32;       // columns per wavefront
   static constexpr int RBW = RB / WROW, NB = RBW * C;      // blocks of rows per wavefront
   static constexpr int AL = HR / 8 / NW, BL = BN / 8 / NW; // loads per wavefront and block of k
-  static constexpr int AB = HR * 128, BB = BN * 128, SCB = NW * 256;     // bytes of a stage: h, W, scales
-  static constexpr int LDS = S * (AB + BB + SCB);
-  static constexpr int ALL = AL + BL + 1;
-  static_assert((CW == 32 || CW == 64) && RBW * WROW == RB && AL * NW * 8 == HR && BL * NW * 8 == BN, "tile shape");
-  static_assert(LDS <= 160 * 1024 && NW * 64 >= HR + BN / 128 + 2 && S >= 2 && (S - 1) * ALL <= 63, "LDS, loads in flight");
+  static constexpr int AB = HR * 128, BB = BN * 128;       // bytes of a stage: h, W
+  static constexpr int ALL = AL + BL;
+  // Scales of h come four blocks at a time, SL loads per wavefront, behind the stages.
+  static constexpr int SL = HR / 16 / NW, GB = HR * 16, GROUPS = (S + 3) / 4 + 1;
+  static constexpr int LDS = S * (AB + BB) + GROUPS * GB;
+  static_assert((CW == 32 || CW == 64) && RBW * WROW == RB && AL * NW * 8 == HR && BL * NW * 8 == BN && SL * NW * 16 == HR, "tile shape");
+  static_assert(LDS <= 160 * 1024 && S >= 2 && (S - 1) * ALL <= 63, "LDS, loads in flight");
 };
 
 struct Fp8Args {
@@ -59,11 +61,12 @@ struct Fp8Args {
   int v_lo;
 };
 
-// 4 bytes per lane from a lane's own address to LDS byte address lds + 4 * lane
+// 4 bytes per lane from base + off (per lane) to LDS byte address lds + ADD + 4 * lane
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_lds4(uint64_t from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+template <int ADD>
+__device__ __forceinline__ void load_lds4(uint64_t base, uint32_t off, uint32_t lds) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base), "n"(ADD) : "memory", "m0", "scc");
 }
 #pragma clang diagnostic pop
 
@@ -82,7 +85,9 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   const int rows = a.B * a.L, d = a.d, KT = (d + 127) / 128, G = KT;
   const int nch = d % 128 / 16;                          // 16-byte chunks of a ragged last block, 0: there is none
   const int p_base = mt * RB * 32;
-  const int col_base = wt * K::BN;                       // columns are counted from the first allowed id
+  // columns are counted from the first allowed id, or from the multiple of 4 before it: a group of the table does not end among the four
+  // columns of a quarter of a lane's registers then
+  const int skip = BORDERS ? f.v_lo % 4 : 0, col_base = wt * K::BN - skip;
   RowState mine[K::RBW];
 #pragma unroll
   for (int i = 0; i < K::RBW; ++i) mine[i] = row_state(a, p_base + (wr * K::RBW + i) * 32 + ln);
@@ -94,7 +99,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   auto odd_piece = [&](int per_wave, int i) { return per_wave % 2 == 0 ? i & 1 : (wave * per_wave + i) & 1; };
   const int h0 = first_h_row(p_base, C, a.L);
   const uint64_t hbase = reinterpret_cast<uint64_t>(a.h) + static_cast<uint64_t>(h0) * d;
-  const int w0 = f.v_lo + col_base, w_last = f.v_lo + a.n - 1;       // first row of W, and the last one that may be read
+  const int w0 = f.v_lo + col_base, w_last = f.v_lo + a.n - 1;       // row of W of the first column, and the last row that may be read
   const uint64_t wbase = reinterpret_cast<uint64_t>(f.W) + static_cast<uint64_t>(w0) * d;
   auto row_of_h = [&](int r) {                           // of row r of the tile: [RB][C][32]
     const int blk = r / 32, rb = blk / C;
@@ -109,17 +114,17 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
   for (int i = 0; i < BL; ++i) {
     const int r = piece_row(BL, i);
-    bo[i] = static_cast<uint32_t>(min(w0 + r, w_last) - w0) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(BL, i)) * 16;
+    bo[i] = static_cast<uint32_t>(min(max(w0 + r, f.v_lo), w_last) - w0) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(BL, i)) * 16;
   }
-  // a word per thread: the scales of h's rows, then those of the columns' groups of 128
-  uint64_t so;
-  if (tid < K::HR) so = reinterpret_cast<uint64_t>(f.h_scales) + static_cast<uint64_t>(row_of_h(tid)) * G * 4;
-  else {
-    const int group = w0 / 128 + min(tid - K::HR, K::BN / 128 + 1);
-    so = reinterpret_cast<uint64_t>(f.W_scales) + static_cast<uint64_t>(min(group, w_last / 128)) * G * 4;
-  }
+  // scales of 16 rows x 4 blocks of k to a load
+  const uint64_t sbase = reinterpret_cast<uint64_t>(f.h_scales) + static_cast<uint64_t>(h0) * G * 4;
+  uint32_t so[K::SL];
+#pragma unroll
+  for (int i = 0; i < K::SL; ++i)
+    so[i] = static_cast<uint32_t>(row_of_h((wave * K::SL + i) * 16 + (lane >> 2)) - h0) * static_cast<uint32_t>(G) * 4u;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)lds));
-  const uint32_t ldsB = lds0 + wave * BL * 1024, ldsA = lds0 + S * K::BB + wave * AL * 1024, ldsS = lds0 + S * (K::BB + K::AB) + wave * 256;
+  const uint32_t ldsB = lds0 + wave * BL * 1024, ldsA = lds0 + S * K::BB + wave * AL * 1024,
+                 ldsS = lds0 + S * (K::BB + K::AB) + wave * K::SL * 256;
 
   // Blocks are walked cyclically, from one that depends on the workgroup: rows are d bytes apart, and workgroups that all begin at block 0
   // ask the same few channels of the L2 for theirs.
@@ -137,14 +142,19 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   // Load q of block t.
   auto load = [&](auto qq, int t, uint32_t stage) {
     constexpr int Q = decltype(qq)::value;
-    if constexpr (Q < AL + BL) {
-      constexpr bool H = Q < AL;
-      constexpr int I = H ? Q : Q - AL;
-      load_lds16<!H && K::NT, I * 1024>((H ? hbase : wbase) + static_cast<uint64_t>(t) * 128, H ? ao[H ? I : 0] : bo[H ? 0 : I],
-                                  H ? ldsA + stage * K::AB : ldsB + stage * K::BB);
-    } else {
-      load_lds4(so + static_cast<uint64_t>(t) * 4, ldsS + stage * K::SCB);
-    }
+    constexpr bool H = Q < AL;
+    constexpr int I = H ? Q : Q - AL;
+    load_lds16<!H && K::NT, I * 1024>((H ? hbase : wbase) + static_cast<uint64_t>(t) * 128, H ? ao[H ? I : 0] : bo[H ? 0 : I],
+                                      H ? ldsA + stage * K::AB : ldsB + stage * K::BB);
+  };
+  // With the u-th block of the walk, where u is a multiple of 4: the scales of four blocks from there on.
+  auto load_scales = [&](int u) __attribute__((always_inline)) {
+    if (u % 4 != 0) return;
+    int k = rot + min(u + (lane & 3), KT - 1);
+    k = k >= KT ? k - KT : k;
+    static_for<K::SL>([&](auto i) {
+      load_lds4<decltype(i)::value * 256>(sbase, so[decltype(i)::value] + static_cast<uint32_t>(k) * 4u, ldsS + u / 4 % K::GROUPS * K::GB);
+    });
   };
   // What a ragged last block lacks counts as 0: in h, by the wavefront that has loaded it.
   auto clear_end = [&](int t, uint32_t stage) {
@@ -157,13 +167,16 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 
   const unsigned char* const Bt = lds + (wc * K::CW + ln) * 128;
   const unsigned char* const At = lds + S * K::BB + (wr * NB * 32 + ln) * 128;
-  const float* const St = reinterpret_cast<const float*>(lds + S * K::BB + S * K::AB);
+  const float* const St = reinterpret_cast<const float*>(lds + S * (K::BB + K::AB)) + (wr * NB * 32 + ln) * 4;
   u32x4 raw[2][NB + NC];                                  // codes of two chunks: NB blocks of rows, then NC of columns
   f16x8 op[2][NB + NC];                                   // operands of two MFMA steps
   f32x16 total[NC][NB], acc[NC][NB];
   // The wavefront's columns lie in one group of 128 of the table, or in two: those from `border` on have the second scale.
   const int first = w0 + wc * K::CW, border = 128 - first % 128;
   float scale[NB], scale2[NB], sw = 0.f, sw2 = 0.f;
+  const uint64_t wscales = reinterpret_cast<uint64_t>(f.W_scales) + static_cast<uint64_t>(min(first, w_last) / 128) * G * 4;
+  const int64_t more = min(first, w_last) / 128 < w_last / 128 ? G : 0;
+  int block_k = rot;                                      // the block of the walk's t-th step
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -183,14 +196,11 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     for (int f = decltype(from)::value; f < decltype(to)::value; ++f) op[E][f] = to_f16(raw[Q & 1][f][2 * E], raw[Q & 1][f][2 * E + 1]);
   };
   auto add_up = [&](int c, int i) __attribute__((always_inline)) {       // the last block's sums, under its scale
-    if (BORDERS && border > c * 32 && border < c * 32 + 32) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        total[c][i][e] = __fmaf_rn(acc[c][i][e], c * 32 + e / 4 * 8 + lg * 4 + e % 4 < border ? scale[i] : scale2[i], total[c][i][e]);
-    } else {
-      const float s = !BORDERS || border > c * 32 ? scale[i] : scale2[i];
+    for (int q = 0; q < 4; ++q) {                         // (four neighbouring columns each)
+      const float s = !BORDERS || c * 32 + q * 8 + lg * 4 < border ? scale[i] : scale2[i];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) total[c][i][e] = __fmaf_rn(acc[c][i][e], s, total[c][i][e]);
+      for (int e = q * 4; e < q * 4 + 4; ++e) total[c][i][e] = __fmaf_rn(acc[c][i][e], s, total[c][i][e]);
     }
   };
 
@@ -204,7 +214,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
       constexpr int X = decltype(which)::value, Q = X / 2, E = X % 2;
       if constexpr (X == 6 && !LAST) {
         hard_fence();
-        if (t + S - 1 < KT) wait_loads<(S - 2) * K::ALL>();      // blocks t + 2 .. t + S - 1 may be on their way
+        if (t + S - 1 < KT) wait_loads<(S - 2) * K::ALL>();      // h and W of blocks t + 2 .. t + S - 1 may be on their way
         else wait_loads<0>();
         clear_end(coming, next);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -213,11 +223,13 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
       }
       if constexpr (E == 0 && !(LAST && Q == 3)) fetch(IntT<(Q + 1) % 4>{}, Q == 3 ? next : stage);
       if constexpr (X == 4) {
-        const float* const at = St + stage * (K::SCB / 4) + K::HR + (first / 128 - w0 / 128);
-        sw = at[0];
-        if (BORDERS) sw2 = at[1];
+        const float* const at = St + t / 4 % K::GROUPS * (K::GB / 4) + t % 4;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) scale[i] = St[stage * (K::SCB / 4) + (wr * NB + i) * 32 + ln];
+        for (int i = 0; i < NB; ++i) scale[i] = at[i * 128];
+        // W's, alike for the whole wavefront, by way of the scalar cache: there before the seventh step, which waits for all of these
+        const auto* const column = reinterpret_cast<const __attribute__((address_space(4))) float*>(wscales);
+        sw = column[block_k];
+        if (BORDERS) sw2 = column[more + block_k];
       }
       __builtin_amdgcn_sched_barrier(0);
       constexpr int NM = NC * NB, NF = NB + NC;
@@ -229,7 +241,10 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (X >= 6 && !LAST) {
           constexpr int SLOT = (X - 6) * NM + M, FROM = K::ALL * SLOT / (2 * NM), TO = K::ALL * (SLOT + 1) / (2 * NM);
-          if (TO > FROM && t + S < KT) static_for<TO - FROM>([&](auto j) { load(IntT<FROM + decltype(j)::value>{}, loaded, stage); });
+          if (t + S < KT) {
+            if constexpr (SLOT == 0) load_scales(t + S);
+            static_for<TO - FROM>([&](auto j) { load(IntT<FROM + decltype(j)::value>{}, loaded, stage); });
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
         constexpr int FROM = NF * M / NM, TO = NF * (M + 1) / NM;
@@ -255,6 +270,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     constexpr int T = decltype(t)::value;
     if (T < KT) {
       ragged_end(loaded, false);
+      load_scales(T);
       static_for<K::ALL>([&](auto q) { load(q, loaded, T); });
       ragged_end(loaded, true);
       loaded = after(loaded);
@@ -275,6 +291,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     const uint32_t next = stage + 1 == S ? 0 : stage + 1;
     block(t, coming, loaded, stage, next, FalseT{});
     stage = next;
+    block_k = coming;
     coming = after(coming);
     loaded = after(loaded);
   }
@@ -299,11 +316,11 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           z[e] = processed_logit<C>(a, total[c][i * C][q * 4 + e], total[c][i * C + C - 1][q * 4 + e]);
-        if (col + 3 < a.n) store4(row + col, z[0], z[1], z[2], z[3]);
+        if (col >= 0 && col + 3 < a.n) store4(row + col, z[0], z[1], z[2], z[3]);
         else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (col + e < a.n) row[col + e] = z[e];
+            if (col + e >= 0 && col + e < a.n) row[col + e] = z[e];
         }
       }
   }
@@ -313,12 +330,12 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 template <class K, class F>
 void with(F&& go) { go(K{}); }
 template <class K>
-int64_t tiles_of(const LmHeadArgs& a) {
-  return ((static_cast<int64_t>(a.n) + K::BN - 1) / K::BN) * ((static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32));
+int64_t tiles_of(const LmHeadArgs& a, int v_lo) {
+  return ((v_lo % 4 + static_cast<int64_t>(a.n) + K::BN - 1) / K::BN) * ((static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32));
 }
 
 template <int C, class F>
-void choose_of(const LmHeadArgs& a, F&& go) {
+void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
   using Large = Fp8Cfg<C, 8 / C, 128, 2, 4, 3>;            // one workgroup on a compute unit
   using Medium = Fp8Cfg<C, 4 / C, 128, 2, 2, 2>;           // two
   using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;              // two
@@ -327,21 +344,21 @@ void choose_of(const LmHeadArgs& a, F&& go) {
   // W is read once, and larger than what the last cache keeps from one call to the next
   const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
   if (rows > 128) {
-    const int64_t large = (tiles_of<Large>(a) + 255) / 256, medium = (tiles_of<Medium>(a) + 511) / 512;
+    const int64_t large = (tiles_of<Large>(a, v_lo) + 255) / 256, medium = (tiles_of<Medium>(a, v_lo) + 511) / 512;
     large <= medium ? with<Large>(go) : with<Medium>(go);
   } else if (rows > 64) {
     past ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, true>>(go) : with<Medium>(go);
   } else if (rows > 32 || C == 2) {
-    if (tiles_of<FewDeep>(a) <= 256) with<FewDeep>(go);
+    if (tiles_of<FewDeep>(a, v_lo) <= 256) with<FewDeep>(go);
     else past ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, true>>(go) : with<Few>(go);
   } else if constexpr (C == 1) {
-    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 8>>(a) <= 256) with<Fp8Cfg<1, 1, 64, 2, 1, 8>>(go);
+    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 8>>(a, v_lo) <= 256) with<Fp8Cfg<1, 1, 64, 2, 1, 8>>(go);
     else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
   }
 }
 template <class F>
-void choose(const LmHeadArgs& a, F&& go) {
-  a.C == 2 ? choose_of<2>(a, go) : choose_of<1>(a, go);
+void choose(const LmHeadArgs& a, int v_lo, F&& go) {
+  a.C == 2 ? choose_of<2>(a, v_lo, go) : choose_of<1>(a, v_lo, go);
 }
 
 // ---- weights in 8 bits ---------------------------------------------------------------------------------------------
@@ -381,17 +398,17 @@ struct Grid {
   int64_t WT, MT, groups;
 };
 template <class K>
-Grid grid_of(const LmHeadArgs& a) {
-  const int64_t WT = (static_cast<int64_t>(a.n) + K::BN - 1) / K::BN, MT = (static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32);
+Grid grid_of(const LmHeadArgs& a, int v_lo) {
+  const int64_t WT = (v_lo % 4 + static_cast<int64_t>(a.n) + K::BN - 1) / K::BN, MT = (static_cast<int64_t>(a.B) * a.L + K::RB * 32 - 1) / (K::RB * 32);
   return {WT, MT, (WT + 7) / 8 * 8 * MT};
 }
 }  // namespace
 
-bool lm_head_fp8_fits(const LmHeadArgs& a) {
+bool lm_head_fp8_fits(const LmHeadArgs& a, int v_lo) {
   bool fits = false;
-  choose(a, [&](auto k) {
+  choose(a, v_lo, [&](auto k) {
     using K = decltype(k);
-    fits = grid_of<K>(a).groups * K::THREADS < static_cast<int64_t>(1) << 32;      // a launch's threads
+    fits = grid_of<K>(a, v_lo).groups * K::THREADS < static_cast<int64_t>(1) << 32;      // a launch's threads
   });
   return fits;
 }
@@ -400,9 +417,9 @@ hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const 
                               hipEvent_t ev_start, hipEvent_t ev_stop) {
   const LaunchEvents ev{ev_start, ev_stop};
   const Fp8Args f{a, h_scales, W, W_scales, v_lo};
-  choose(a, [&](auto k) {
+  choose(a, v_lo, [&](auto k) {
     using K = decltype(k);
-    const Grid g = grid_of<K>(a);
+    const Grid g = grid_of<K>(a, v_lo);
     launch_kernel(v_lo % 64 != 0 ? lm_head_fp8_kernel<K, true> : lm_head_fp8_kernel<K, false>, dim3(static_cast<unsigned>(g.groups)),
                   dim3(K::THREADS), s, ev, f, static_cast<int>(g.WT), static_cast<int>(g.MT));
   });
@@ -411,7 +428,7 @@ hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const 
 
 int lm_head_fp8_kernel_name(const LmHeadArgs& a, int v_lo, char* buf, size_t cap) {
   int len = 0;
-  choose(a, [&](auto k) { len = decltype(k)::name(buf, cap, v_lo % 64 != 0); });
+  choose(a, v_lo, [&](auto k) { len = decltype(k)::name(buf, cap, v_lo % 64 != 0); });
   return len;
 }
 

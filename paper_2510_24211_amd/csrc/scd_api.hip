@@ -417,7 +417,7 @@ int fp8_args(scd_ctx* c, const uint8_t* d_h, const float* d_h_scales, const uint
   a->lam = c->cfg.cfg_lambda;
   a->one_plus_lam = 1.0f + c->cfg.cfg_lambda;
   a->tau = c->cfg.temperature;
-  return scd::lm_head_fp8_fits(*a) ? SCD_OK : SCD_EUNSUPPORTED;
+  return scd::lm_head_fp8_fits(*a, c->cfg.v_lo) ? SCD_OK : SCD_EUNSUPPORTED;
 }
 
 // The list as the launchers take it, in host memory of its own.
@@ -780,7 +780,7 @@ int scd_lm_head_fp8_kernel_name(scd_ctx* c, char* host_buf, size_t cap) {
   if (!c || !host_buf || c->cfg.d <= 0) return SCD_EINVAL;
   scd::LmHeadArgs a{};
   a.B = c->cfg.B; a.C = c->C; a.L = c->cfg.L; a.d = c->cfg.d; a.n = c->n;
-  if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20) || c->n > kMostIds || !scd::lm_head_fp8_fits(a)) return SCD_EUNSUPPORTED;
+  if (c->cfg.d % 16 != 0 || c->cfg.d > (1 << 20) || c->n > kMostIds || !scd::lm_head_fp8_fits(a, c->cfg.v_lo)) return SCD_EUNSUPPORTED;
   return static_cast<size_t>(scd::lm_head_fp8_kernel_name(a, c->cfg.v_lo, host_buf, cap)) >= cap ? SCD_EINVAL : SCD_OK;
 }
 

@@ -239,8 +239,8 @@ int lm_head_quantized_kernel_name(const LmHeadArgs& a, int group, bool zeros, ch
 hipError_t launch_quantize_fp8(const uint16_t* W, int V, int d, uint8_t* codes, float* scales, hipStream_t s);
 hipError_t launch_lm_head_fp8(const LmHeadArgs& a, const float* h_scales, const uint8_t* W, const float* W_scales, int v_lo, hipStream_t s,
                               hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);      // as in launch_lm_head
-// whether its launch can hold the tiles of a call of these sizes (B, C, L, n are read)
-bool lm_head_fp8_fits(const LmHeadArgs& a);
+// whether its launch can hold the tiles of a call of these sizes (B, C, L, d and n are read)
+bool lm_head_fp8_fits(const LmHeadArgs& a, int v_lo);
 // Name of the kernel that it picks (B, C, L, d and n are read); snprintf semantics.
 int lm_head_fp8_kernel_name(const LmHeadArgs& a, int v_lo, char* buf, size_t cap);
 
