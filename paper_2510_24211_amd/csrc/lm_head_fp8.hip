@@ -30,16 +30,16 @@ __device__ __forceinline__ f16x8 to_f16(uint32_t a, uint32_t b) {
 }
 
 // RB blocks of 32 window rows (times C with guidance) x BN columns by WCOL x WROW wavefronts; S stages
-// NT: W past the caches
-template <int C_, int RB_, int BN_, int WCOL_, int WROW_, int S_, bool NT_ = false>
+// of each of WK parts of k, which have wavefronts and stages of their own; NT: W past the caches
+template <int C_, int RB_, int BN_, int WCOL_, int WROW_, int S_, int WK_ = 1, bool NT_ = false>
 struct Fp8Cfg {
-  static constexpr int C = C_, RB = RB_, BN = BN_, WCOL = WCOL_, WROW = WROW_, S = S_;
+  static constexpr int C = C_, RB = RB_, BN = BN_, WCOL = WCOL_, WROW = WROW_, S = S_, WK = WK_;
   static constexpr bool NT = NT_;
   static int name(char* buf, size_t cap, bool borders) {
-    return snprintf(buf, cap, "lm_head_fp8_kernel<Fp8Cfg<%d, %d, %d, %d, %d, %d, %s>, %s>", C, RB, BN, WCOL, WROW, S, NT ? "true" : "false",
+    return snprintf(buf, cap, "lm_head_fp8_kernel<Fp8Cfg<%d, %d, %d, %d, %d, %d, %d, %s>, %s>", C, RB, BN, WCOL, WROW, S, WK, NT ? "true" : "false",
                     borders ? "true" : "false");
   }
-  static constexpr int NW = WCOL * WROW, THREADS = NW * 64;
+  static constexpr int NW = WCOL * WROW, THREADS = NW * WK * 64;
   static constexpr int HR = RB * C * 32;                   // rows of h
   static constexpr int CW = BN / WCOL, NC = CW / 32;       // columns per wavefront
   static constexpr int RBW = RB / WROW, NB = RBW * C;      // blocks of rows per wavefront
@@ -48,9 +48,10 @@ struct Fp8Cfg {
   static constexpr int ALL = AL + BL;
   // Scales of h come four blocks at a time, SL loads per wavefront, behind the stages.
   static constexpr int SL = HR / 16 / NW, GB = HR * 16, GROUPS = (S + 3) / 4 + 1;
-  static constexpr int LDS = S * (AB + BB) + GROUPS * GB;
+  static constexpr int PART = S * (AB + BB) + GROUPS * GB, LDS = WK * PART;       // LDS of a part of k, of all
+  static constexpr int ACC = NC * NB == 1 ? 2 : 1;         // sums side by side: one alone would have every MFMA wait for the last
   static_assert((CW == 32 || CW == 64) && RBW * WROW == RB && AL * NW * 8 == HR && BL * NW * 8 == BN && SL * NW * 16 == HR, "tile shape");
-  static_assert(LDS <= 160 * 1024 && S >= 2 && (S - 1) * ALL <= 63, "LDS, loads in flight");
+  static_assert(LDS <= 160 * 1024 && PART >= NW * NC * NB * 4096 && S >= 2 && (S - 1) * ALL <= 63, "LDS, loads in flight");
 };
 
 struct Fp8Args {
@@ -74,15 +75,18 @@ __device__ __forceinline__ void load_lds4(uint64_t base, uint32_t off, uint32_t 
 template <class K, bool BORDERS>
 __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void lm_head_fp8_kernel(const Fp8Args f, const int WT, const int MT) {
   constexpr int C = K::C, RB = K::RB, NB = K::NB, NC = K::NC, AL = K::AL, BL = K::BL, S = K::S;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[K::LDS];      // W's stages, then h's, then the scales'
+  __shared__ __attribute__((aligned(1024))) unsigned char whole[K::LDS];    // for each part of k: W's stages, then h's, then the scales'
   const LmHeadArgs& a = f.lm;
   // workgroups that share columns get ids 8 apart: the same XCD, the same L2
   const int id = blockIdx.x, mt = (id / 8) % MT, wt = id / (8 * MT) * 8 + id % 8;
   if (wt >= WT) return;
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lg = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = K::WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6) / K::NW;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) - part * K::NW;
   const int wc = wave % K::WCOL, wr = wave / K::WCOL;
+  unsigned char* const lds = whole + part * K::PART;
   const int rows = a.B * a.L, d = a.d, KT = (d + 127) / 128, G = KT;
+  const int k0 = KT * part / K::WK, count = KT * (part + 1) / K::WK - k0;      // the part's blocks of k; KT >= WK
   const int nch = d % 128 / 16;                          // 16-byte chunks of a ragged last block, 0: there is none
   const int p_base = mt * RB * 32;
   // columns are counted from the first allowed id, or from the multiple of 4 before it: a group of the table does not end among the four
@@ -128,8 +132,8 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 
   // Blocks are walked cyclically, from one that depends on the workgroup: rows are d bytes apart, and workgroups that all begin at block 0
   // ask the same few channels of the L2 for theirs.
-  const int rot = (MT > 1 ? id % 8 : wt) * 5 % KT;
-  auto after = [&](int k) { return k + 1 == KT ? 0 : k + 1; };
+  const int rot = k0 + (MT > 1 ? id % 8 : wt) * 5 % count;
+  auto after = [&](int k) { return k + 1 == k0 + count ? k0 : k + 1; };
   // Past a ragged end a row's last chunk is read: offsets of the loads of block KT - 1, made before them and taken back behind.
   auto ragged_end = [&](int t, bool back) __attribute__((always_inline)) {
     if (t != KT - 1 || nch == 0) return;
@@ -150,8 +154,8 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   // With the u-th block of the walk, where u is a multiple of 4: the scales of four blocks from there on.
   auto load_scales = [&](int u) __attribute__((always_inline)) {
     if (u % 4 != 0) return;
-    int k = rot + min(u + (lane & 3), KT - 1);
-    k = k >= KT ? k - KT : k;
+    int k = rot + min(u + (lane & 3), count - 1);
+    k = k >= k0 + count ? k - count : k;
     static_for<K::SL>([&](auto i) {
       load_lds4<decltype(i)::value * 256>(sbase, so[decltype(i)::value] + static_cast<uint32_t>(k) * 4u, ldsS + u / 4 % K::GROUPS * K::GB);
     });
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   const float* const St = reinterpret_cast<const float*>(lds + S * (K::BB + K::AB)) + (wr * NB * 32 + ln) * 4;
   u32x4 raw[2][NB + NC];                                  // codes of two chunks: NB blocks of rows, then NC of columns
   f16x8 op[2][NB + NC];                                   // operands of two MFMA steps
-  f32x16 total[NC][NB], acc[NC][NB];
+  f32x16 total[NC][NB], acc[K::ACC][NC][NB];
   // The wavefront's columns lie in one group of 128 of the table, or in two: those from `border` on have the second scale.
   const int first = w0 + wc * K::CW, border = 128 - first % 128;
   float scale[NB], scale2[NB], sw = 0.f, sw2 = 0.f;
@@ -200,7 +204,8 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     for (int q = 0; q < 4; ++q) {                         // (four neighbouring columns each)
       const float s = !BORDERS || c * 32 + q * 8 + lg * 4 < border ? scale[i] : scale2[i];
 #pragma unroll
-      for (int e = q * 4; e < q * 4 + 4; ++e) total[c][i][e] = __fmaf_rn(acc[c][i][e], s, total[c][i][e]);
+      for (int e = q * 4; e < q * 4 + 4; ++e)
+        total[c][i][e] = __fmaf_rn(K::ACC == 2 ? acc[0][c][i][e] + acc[K::ACC - 1][c][i][e] : acc[0][c][i][e], s, total[c][i][e]);
     }
   };
 
@@ -214,7 +219,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
       constexpr int X = decltype(which)::value, Q = X / 2, E = X % 2;
       if constexpr (X == 6 && !LAST) {
         hard_fence();
-        if (t + S - 1 < KT) wait_loads<(S - 2) * K::ALL>();      // h and W of blocks t + 2 .. t + S - 1 may be on their way
+        if (t + S - 1 < count) wait_loads<(S - 2) * K::ALL>();      // h and W of blocks t + 2 .. t + S - 1 may be on their way
         else wait_loads<0>();
         clear_end(coming, next);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -237,11 +242,12 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
       static_for<NM>([&](auto mm) {
         constexpr int M = decltype(mm)::value, c = M / NB, i = M % NB;
         if constexpr (X == 0 && !FIRST) add_up(c, i);
-        acc[c][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[E][NB + c], op[E][i], X == 0 ? f32x16{} : acc[c][i], 0, 0, 0);
+        f32x16& sum = acc[K::ACC == 2 ? E : 0][c][i];
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(op[E][NB + c], op[E][i], X < K::ACC ? f32x16{} : sum, 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (X >= 6 && !LAST) {
           constexpr int SLOT = (X - 6) * NM + M, FROM = K::ALL * SLOT / (2 * NM), TO = K::ALL * (SLOT + 1) / (2 * NM);
-          if (t + S < KT) {
+          if (t + S < count) {
             if constexpr (SLOT == 0) load_scales(t + S);
             static_for<TO - FROM>([&](auto j) { load(IntT<FROM + decltype(j)::value>{}, loaded, stage); });
           }
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   int loaded = rot, coming = after(rot);                  // blocks to be loaded next, and to be multiplied next but one
   static_for<S>([&](auto t) {
     constexpr int T = decltype(t)::value;
-    if (T < KT) {
+    if (T < count) {
       ragged_end(loaded, false);
       load_scales(T);
       static_for<K::ALL>([&](auto q) { load(q, loaded, T); });
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
       loaded = after(loaded);
     }
   });
-  if (KT >= S) wait_loads<(S - 1) * K::ALL>();
+  if (count >= S) wait_loads<(S - 1) * K::ALL>();
   else wait_loads<0>();
   clear_end(rot, 0);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -287,7 +293,7 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   step(IntT<0>{}, 0, 0, 0, 0, 0, TrueT{}, FalseT{});
   uint32_t stage = 0;
 #pragma unroll 1
-  for (int t = 0; t < KT - 1; ++t) {
+  for (int t = 0; t < count - 1; ++t) {
     const uint32_t next = stage + 1 == S ? 0 : stage + 1;
     block(t, coming, loaded, stage, next, FalseT{});
     stage = next;
@@ -295,11 +301,40 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     coming = after(coming);
     loaded = after(loaded);
   }
-  block(KT - 1, 0, 0, stage, stage, TrueT{});
+  block(count - 1, 0, 0, stage, stage, TrueT{});
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int i = 0; i < NB; ++i) add_up(c, i);
+  if constexpr (K::WK > 1) {
+    // the parts of k are joined in the stages' place, in order
+    if (count < (KT + K::WK - 1) / K::WK) __builtin_amdgcn_s_barrier();        // a block less: the others have one more of its barriers
+    f32x4* const sums = reinterpret_cast<f32x4*>(whole) + (wave * NC * NB * 4) * 64 + lane;
+    constexpr int STRIDE = K::NW * NC * NB * 4 * 64;
+    __syncthreads();
+    if (part > 0) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            sums[(part - 1) * STRIDE + ((c * NB + i) * 4 + q) * 64] = f32x4{total[c][i][q * 4], total[c][i][q * 4 + 1], total[c][i][q * 4 + 2], total[c][i][q * 4 + 3]};
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int p = 0; p < K::WK - 1; ++p)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 v = sums[p * STRIDE + ((c * NB + i) * 4 + q) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) total[c][i][q * 4 + e] += v[e];
+          }
+  }
 
   // ---- logits: a lane has a window row, a register a column --------------------------------------------------
 #pragma unroll
@@ -339,7 +374,7 @@ void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
   using Large = Fp8Cfg<C, 8 / C, 128, 2, 4, 3>;            // one workgroup on a compute unit
   using Medium = Fp8Cfg<C, 4 / C, 128, 2, 2, 2>;           // two
   using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;              // two
-  using FewDeep = Fp8Cfg<C, 2 / C, 64, 2, 1, 6>;           // one
+  using FewParts = Fp8Cfg<C, 2 / C, 64, 2, 1, 2, 4>;       // one
   const int64_t rows = static_cast<int64_t>(a.B) * a.L * C;
   // W is read once, and larger than what the last cache keeps from one call to the next
   const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
@@ -347,13 +382,13 @@ void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
     const int64_t large = (tiles_of<Large>(a, v_lo) + 255) / 256, medium = (tiles_of<Medium>(a, v_lo) + 511) / 512;
     large <= medium ? with<Large>(go) : with<Medium>(go);
   } else if (rows > 64) {
-    past ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, true>>(go) : with<Medium>(go);
+    past ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, 1, true>>(go) : with<Medium>(go);
   } else if (rows > 32 || C == 2) {
-    if (tiles_of<FewDeep>(a, v_lo) <= 256) with<FewDeep>(go);
-    else past ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, true>>(go) : with<Few>(go);
+    if (tiles_of<FewParts>(a, v_lo) <= 256 && a.d > 384) with<FewParts>(go);
+    else past ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, 1, true>>(go) : with<Few>(go);
   } else if constexpr (C == 1) {
-    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 8>>(a, v_lo) <= 256) with<Fp8Cfg<1, 1, 64, 2, 1, 8>>(go);
-    else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
+    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(a, v_lo) <= 256 && a.d > 384) with<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(go);
+    else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, 1, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
   }
 }
 template <class F>
