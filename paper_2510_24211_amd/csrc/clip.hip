@@ -3,6 +3,10 @@
 // The tensors (their addresses, sizes and types) travel in the kernel's arguments, kTensors to a launch: nothing has to be copied to the
 // card first, and a recorded graph holds them.  Chunks of kChunk elements are dealt to the workgroups; squares are added up in 64 bits
 // (they are exact there: no range is lost, and the unit that adds them is idle otherwise), the workgroups' sums in order by a last one.
+//   Bound by memory, each gradient being read twice: the norm has to be known first.  Clipping goes backwards, so that it begins with what the
+// norm's pass has left in the last cache, and stores past the caches, so that what it writes does not drive that out.  805 million bf16
+// gradients in 50 tensors into bf16: 841 us (4.83 GB: 5.7 TB/s) where forwards and through the caches took 940; 34 million fp32 ones into
+// bf16 62 us, 67 before.  512 workgroups of 64 KB at a time are as fast as any number up to 2048 (841 to 860 us), 4096 with 16 KB take 880.
 #include <algorithm>
 
 #include "eights.h"
@@ -13,8 +17,8 @@ namespace scd {
 namespace {
 
 constexpr int kTensors = 100;                    // (the arguments of a launch end at 4 KB)
-constexpr int kUnroll = 4, kChunk = 256 * 8 * kUnroll;
-constexpr int kGroups = 2048;                    // workgroups of a launch: all that run at once
+constexpr int kUnroll = 8, kChunk = 256 * 8 * kUnroll;
+constexpr int kGroups = 512;                     // workgroups of a launch
 
 struct Table {
   const void* in[kTensors];
@@ -63,10 +67,10 @@ template <bool F32>
 __device__ __forceinline__ void put_any(void* p, int64_t at, f32x8 v) {
   if constexpr (F32) {
     float* const q = static_cast<float*>(p) + at;
-    *reinterpret_cast<f32x4_any*>(q) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_any*>(q + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_any*>(q));
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_any*>(q + 4));
   } else {
-    *reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(p) + at) = narrow(v);
+    __builtin_nontemporal_store(narrow(v), reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(p) + at));
   }
 }
 template <bool F32>
@@ -146,7 +150,8 @@ __global__ __launch_bounds__(256) void clip_kernel(const Table t, float most, co
   const float have = norm[0];
   const float by = have <= most ? 1.f : __fdiv_rn(most, have);        // (a NaN for a NaN)
   const uint32_t chunks = t.first[t.count];
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+  for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+    const uint32_t c = chunks - 1 - i;
     const int k = tensor_of(t, c);
     const bool in_f32 = t.in_f32[k], out_f32 = t.out_f32[k];
     void* const out = t.out[k];

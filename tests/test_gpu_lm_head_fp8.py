@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+from fp8_shapes import CASES, MORE
 from oracle import scd as oscd
 from paper_2510_24211_amd import binding as B
 
@@ -59,16 +60,7 @@ def _want(h, hs, W, Ws, c):
     return z / tau, b / tau + 3 * U * z.abs() / tau
 
 
-CASES = [  # B, L, lam, V, v_lo, n, d, tau
-    (1, 1, 0.0, 1, 0, 1, 16, 1.0), (1, 1, 0.0, 40, 3, 33, 128, 1.0), (1, 1, 3.0, 300, 0, 300, 144, 1.0), (1, 5, 0.0, 300, 127, 130, 208, 0.5),
-    (1, 8, 2.0, 700, 129, 511, 112, 1.0), (2, 20, 3.0, 515, 5, 510, 272, 0.9), (1, 33, 0.0, 2000, 250, 1749, 1296, 1.0),
-    (3, 32, 3.0, 1000, 40, 900, 528, 1.0), (1, 64, 0.0, 31, 0, 31, 4096, 1.0), (5, 26, 0.0, 1285, 0, 1285, 1312, 1.0), (7, 1, 0.0, 9000, 1000, 7999, 640, 1.0),
-    (9, 31, 3.0, 300, 1, 299, 144, 0.8), (3, 64, 0.0, 515, 0, 500, 720, 1.0), (2, 150, 0.0, 200, 10, 130, 256, 1.0), (1, 129, 0.0, 64, 0, 64, 64, 1.0),
-    (5, 30, 2.0, 1260, 128, 1130, 7008, 1.0), (40, 1, 3.0, 2100, 77, 2000, 384, 1.0), (2, 16, 3.0, 40000, 300, 39000, 512, 1.0),
-    (1, 2, 0.0, 70000, 0, 70000, 2048, 1.0), (300, 2, 0.0, 3000, 255, 2700, 1024, 1.0), (100, 3, 1.5, 3000, 255, 2700, 1152, 1.0)]
-
-
-@pytest.mark.parametrize("Bn,L,lam,V,v_lo,n,d,tau", CASES)
+@pytest.mark.parametrize("Bn,L,lam,V,v_lo,n,d,tau", CASES + MORE)
 def test_logits(Bn, L, lam, V, v_lo, n, d, tau):
     s = B.Scd(B.make_config(B=Bn, L=L, N=L, V=V, d=d, v_lo=v_lo, v_hi=v_lo + n, cfg_lambda=lam, temperature=tau))
     W, Ws = _table(V, d, seed=n + d)
