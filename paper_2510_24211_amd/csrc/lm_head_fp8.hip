@@ -9,8 +9,17 @@
 // converted, two by an instruction, on their way from LDS to the MFMAs.
 //
 // Rows of h are the MFMA's columns: a lane has one row, and one scale of it; its columns' scale is one number, or two where a group of the
-// table ends among them.  h, W and the scales go from memory straight into LDS, 128 bytes of a
-// row to a stage; slot l % 8 of row l / 8 of a load holds chunk (l % 8) ^ ((row >> 1) & 7): operand reads are then free of bank conflicts.
+// table ends among them.  h, W and the scales of h go from memory straight into LDS, 128 bytes of a row to a stage; slot l % 8 of row l / 8 of a
+// load holds chunk (l % 8) ^ ((row >> 1) & 7): operand reads are then free of bank conflicts.  Scales of h come for four blocks at a time (a word
+// per row and block would ask the L2 for as many lines as h and W together: 5 % of the time), W's by way of the scalar cache.
+//
+//   What bounds it (d = 4096, guidance).  Few rows: memory.  One row x 65536 ids takes 45 us (268 MB of W: 6.0 TB/s), 32 x 2 rows 54; the bf16 head
+// takes 82 for the latter.  Many rows: the matrix pipes at the clock that they leave the card.  512 x 2 rows x 8192 ids, one round of tiles, take
+// 61 to 63 us; with every vector instruction and load taken out of the loop 52 to 54 remain, which is 1.43 PFLOP/s behind some 8 us of
+// launch, first loads and stores, the rate of a large product of 16 bits.  512 x 2 x 64000 takes 490 to 510 us (1.05 to 1.1 PFLOP/s).  What was
+// tried: loads and conversions ahead of the MFMAs instead of between them 541 us; the sums of a block carried over the loop's end as copies
+// (64 moves, and spilled offsets whose reloads wait for all loads) 880; all workgroups from block 0 on 65 instead of 59 (32 x 2 rows);
+// logits turned in LDS for stores of whole lines: nothing; stores past the caches: 560.
 #include "eights.h"
 #include "launch_events.h"
 #include "lm_head_rows.h"
@@ -371,12 +380,18 @@ int64_t tiles_of(const LmHeadArgs& a, int v_lo) {
 
 template <int C, class F>
 void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
+  // 256 and 128 rows of h: a wavefront has 64 x 64 logits, which keeps its conversions below what the MFMAs hide.  As many compute units'
+  // rounds decide: 480 x 2 rows x 8191 took 73 us in 260 tiles of the larger shape, 86 in 520 of the smaller; alike where both fill their rounds.
   using Large = Fp8Cfg<C, 8 / C, 128, 2, 4, 3>;            // one workgroup on a compute unit
   using Medium = Fp8Cfg<C, 4 / C, 128, 2, 2, 2>;           // two
-  using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;              // two
-  using FewParts = Fp8Cfg<C, 2 / C, 64, 2, 1, 2, 4>;       // one
+  // 64 rows or 32: a stream of W, three stages in each of two or four workgroups on a compute unit.  Where that leaves compute units idle, narrow
+  // tiles with k in four parts (a wavefront's chain of MFMAs is what such a call waits for): 32 x 2 rows x 16384 x 1280 take 10.0 us, 11.1 to 12.6
+  // without parts.
+  using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;
+  using FewParts = Fp8Cfg<C, 2 / C, 64, 2, 1, 2, 4>;
   const int64_t rows = static_cast<int64_t>(a.B) * a.L * C;
-  // W is read once, and larger than what the last cache keeps from one call to the next
+  // W is read once, and larger than what the last cache keeps from one call to the next: past the caches 32 x 2 rows x 65536 x 4096 take 56 us, 58
+  // by way of them, one row 54 and 58 (before other changes)
   const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
   if (rows > 128) {
     const int64_t large = (tiles_of<Large>(a, v_lo) + 255) / 256, medium = (tiles_of<Medium>(a, v_lo) + 511) / 512;
