@@ -193,17 +193,18 @@ def _grad_type(dtype):
 
 
 _E4M3 = (torch.float8_e4m3fn, torch.uint8)
+_F32 = (torch.float32,)
 BF16, F32 = 0, 1
 _TYPE = {torch.bfloat16: BF16, torch.float32: F32}
 
 
-def _type(t, what):
-    """scd_type of a tensor; of none, any."""
-    if t is None:
-        return BF16
-    if not isinstance(t, torch.Tensor) or t.dtype not in _TYPE:
-        raise TypeError(f"{what}: expected a tensor of one of {tuple(_TYPE)}")
-    return _TYPE[t.dtype]
+_TYPES = tuple(_TYPE)
+
+
+def _typed(t, numel, what):
+    """Device address and scd_type of a tensor; of none, any."""
+    p = _ptr(t, _TYPES, numel, what)
+    return p, BF16 if t is None else _TYPE[t.dtype]
 
 
 class TensorList:
@@ -213,7 +214,7 @@ class TensorList:
         self.tensors = list(tensors)
         self.array = (ScdTensor * max(1, len(self.tensors)))()
         for i, t in enumerate(self.tensors):
-            p = _ptr(t, tuple(_TYPE), 0, f"tensor {i}")
+            p = _ptr(t, _TYPES, 0, f"tensor {i}")
             if p is None:
                 raise TypeError(f"tensor {i}: expected a CUDA tensor")
             self.array[i] = ScdTensor(p, t.numel(), _TYPE[t.dtype])
@@ -479,29 +480,26 @@ class Scd:
             raise ValueError(f"{what}: expected a tensor of whole rows of {self.cfg.d}")
         return _int32(t.numel() // max(1, self.cfg.d), what)
 
-    def _norm_stream(self, rows, residual, sum):
-        """Pointers and type of the residual stream before and behind the addition."""
+    def _norm_args(self, x, gain, eps, residual, sum):
+        """What both norms take alike, and the address of the stream behind the addition."""
+        rows, d = self._rows(x, "x"), self.cfg.d
+        n = rows * d
         if residual is not None and sum is not None and residual.dtype != sum.dtype:
             raise TypeError(f"sum: dtype {sum.dtype}, the residual's is {residual.dtype}")
-        n = rows * self.cfg.d
-        return (_ptr(residual, tuple(_TYPE), n, "residual"), _type(residual, "residual"), _ptr(sum, tuple(_TYPE), n, "sum"))
+        return rows, n, (self.ctx, _ptr(x, _BF16, n, "x"), *_typed(residual, n, "residual"), *_typed(gain, d, "gain"), float(eps), rows), _ptr(
+            sum, _TYPES, n, "sum")
 
     def norm(self, x, gain, y, eps, residual=None, sum=None, inv=None):
         """y = s * inv * gain, s = x + residual (kept in sum, which may be residual), inv = 1 / sqrt(mean(s^2) + eps)."""
-        rows = self._rows(x, "x")
-        r, stream, s = self._norm_stream(rows, residual, sum)
-        self._check(self.lib.scd_norm(
-            self.ctx, _ptr(x, _BF16, rows * self.cfg.d, "x"), r, stream, _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
-            float(eps), rows, _ptr(y, _BF16, rows * self.cfg.d, "y"), s, _ptr(inv, (torch.float32,), rows, "inv")), "scd_norm")
+        rows, n, args, s = self._norm_args(x, gain, eps, residual, sum)
+        self._check(self.lib.scd_norm(*args, _ptr(y, _BF16, n, "y"), s, _ptr(inv, _F32, rows, "inv")), "scd_norm")
 
     def norm_fp8(self, x, gain, codes, scales, eps, residual=None, sum=None, inv=None):
         """The same with y as e4m3 codes and a scale per 128 of a row."""
-        rows, G = self._rows(x, "x"), -(-self.cfg.d // 128)
-        r, stream, s = self._norm_stream(rows, residual, sum)
+        rows, n, args, s = self._norm_args(x, gain, eps, residual, sum)
         self._check(self.lib.scd_norm_fp8(
-            self.ctx, _ptr(x, _BF16, rows * self.cfg.d, "x"), r, stream, _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
-            float(eps), rows, _ptr(codes, _E4M3, rows * self.cfg.d, "codes"), _ptr(scales, (torch.float32,), rows * G, "scales"), s,
-            _ptr(inv, (torch.float32,), rows, "inv")), "scd_norm_fp8")
+            *args, _ptr(codes, _E4M3, n, "codes"), _ptr(scales, _F32, rows * -(-self.cfg.d // 128), "scales"), s, _ptr(inv, _F32, rows, "inv")),
+            "scd_norm_fp8")
 
     def norm_backward_workspace(self, rows):
         return self._workspace(self.lib.scd_norm_backward_workspace_bytes(ctypes.byref(self.cfg), _int32(rows, "rows")),
@@ -509,15 +507,16 @@ class Scd:
 
     def norm_backward(self, sum, gain, inv, dy, dx, dgain, workspace, dsum=None, accumulate=False):
         """dx (bf16 or fp32, as dsum): gradient of x and of the residual; dgain (bf16 or fp32, or None) = or += the gains'."""
-        rows = self._rows(sum, "sum")
-        n = rows * self.cfg.d
+        rows, d = self._rows(sum, "sum"), self.cfg.d
+        n = rows * d
         if dsum is not None and dsum.dtype != dx.dtype:
             raise TypeError(f"dsum: dtype {dsum.dtype}, dx's is {dx.dtype}")
+        dx, grad = _typed(dx, n, "dx")
+        dgain, gain_grad = _typed(dgain, d, "dgain")
         self._check(self.lib.scd_norm_backward(
-            self.ctx, _ptr(sum, tuple(_TYPE), n, "sum"), _type(sum, "sum"), _ptr(gain, tuple(_TYPE), self.cfg.d, "gain"), _type(gain, "gain"),
-            _ptr(inv, (torch.float32,), rows, "inv"), _ptr(dy, _BF16, n, "dy"), _ptr(dsum, tuple(_TYPE), n, "dsum"), _type(dx, "dx"), rows,
-            _ptr(dx, tuple(_TYPE), n, "dx"), _ptr(dgain, tuple(_TYPE), self.cfg.d, "dgain"), _type(dgain, "dgain"), int(accumulate),
-            _ptr(workspace, (torch.uint8,), 1, "workspace"), workspace.numel()), "scd_norm_backward")
+            self.ctx, *_typed(sum, n, "sum"), *_typed(gain, d, "gain"), _ptr(inv, _F32, rows, "inv"), _ptr(dy, _BF16, n, "dy"),
+            _ptr(dsum, _TYPES, n, "dsum"), grad, rows, dx, dgain, gain_grad, int(accumulate), _ptr(workspace, (torch.uint8,), 1, "workspace"),
+            workspace.numel()), "scd_norm_backward")
 
     def quantize_fp8(self, W, codes, scales):
         """W as e4m3 codes and a scale for each block of 128 x 128."""
