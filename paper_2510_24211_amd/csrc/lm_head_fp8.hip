@@ -26,6 +26,8 @@
 
 #include <stdio.h>
 
+#include <algorithm>
+
 namespace scd {
 namespace {
 
@@ -380,31 +382,39 @@ int64_t tiles_of(const LmHeadArgs& a, int v_lo) {
 
 template <int C, class F>
 void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
-  // 256 and 128 rows of h: a wavefront has 64 x 64 logits, which keeps its conversions below what the MFMAs hide.  As many compute units'
-  // rounds decide: 480 x 2 rows x 8191 took 73 us in 260 tiles of the larger shape, 86 in 520 of the smaller; alike where both fill their rounds.
+  // 256 and 128 rows of h: a wavefront has 64 x 64 logits, which keeps its conversions below what the MFMAs hide.  64 rows: a stream of W, three
+  // stages in each of two workgroups on a compute unit; narrow tiles with k in four parts where the others leave compute units idle (a
+  // wavefront's chain of MFMAs is what a call of few tiles waits for).
   using Large = Fp8Cfg<C, 8 / C, 128, 2, 4, 3>;            // one workgroup on a compute unit
   using Medium = Fp8Cfg<C, 4 / C, 128, 2, 2, 2>;           // two
-  // 64 rows or 32: a stream of W, three stages in each of two or four workgroups on a compute unit.  Where that leaves compute units idle, narrow
-  // tiles with k in four parts (a wavefront's chain of MFMAs is what such a call waits for): 32 x 2 rows x 16384 x 1280 take 10.0 us, 11.1 to 12.6
-  // without parts.
-  using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;
-  using FewParts = Fp8Cfg<C, 2 / C, 64, 2, 1, 2, 4>;
+  using Few = Fp8Cfg<C, 2 / C, 128, 4, 1, 3>;              // two
+  using FewParts = Fp8Cfg<C, 2 / C, 64, 2, 1, 2, 4>;       // one
   const int64_t rows = static_cast<int64_t>(a.B) * a.L * C;
   // W is read once, and larger than what the last cache keeps from one call to the next: past the caches 32 x 2 rows x 65536 x 4096 take 56 us, 58
   // by way of them, one row 54 and 58 (before other changes)
   const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
-  if (rows > 128) {
-    const int64_t large = (tiles_of<Large>(a, v_lo) + 255) / 256, medium = (tiles_of<Medium>(a, v_lo) + 511) / 512;
-    large <= medium ? with<Large>(go) : with<Medium>(go);
-  } else if (rows > 64) {
-    past ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, 1, true>>(go) : with<Medium>(go);
-  } else if (rows > 32 || C == 2) {
-    if (tiles_of<FewParts>(a, v_lo) <= 256 && a.d > 384) with<FewParts>(go);
-    else past ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, 1, true>>(go) : with<Few>(go);
-  } else if constexpr (C == 1) {
-    if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(a, v_lo) <= 256 && a.d > 384) with<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(go);
-    else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, 1, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
+  if constexpr (C == 1) {
+    if (rows <= 32) {
+      if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(a, v_lo) <= 256 && a.d > 384) with<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(go);
+      else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, 1, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
+      return;
+    }
   }
+  // What rounds of tiles over 256 compute units take, measured at d = 4096 (us, 64 to 512 rows with guidance x 500 to 8000 ids; at d = 1024 they stand
+  // to each other alike): a round of the larger shape 50 to 65, of two smaller tiles per compute unit 67, of one 35 to 42, of two streams 43, of
+  // one 26 to 30, of parts 14 each behind the first.  64 x 2 rows x 1000: 50, 35, 26, 14 us; 512 x 2 x 8000: 65, 67, 83, 111.
+  auto halves = [](int64_t tiles, double two, double one) {
+    const int64_t rest = tiles % 512;
+    return static_cast<double>(tiles / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
+  };
+  const double large = 62.0 * static_cast<double>((tiles_of<Large>(a, v_lo) + 255) / 256), medium = halves(tiles_of<Medium>(a, v_lo), 67.0, 42.0),
+               few = halves(tiles_of<Few>(a, v_lo), 43.0, 29.5),
+               parts = a.d > 384 ? 2.5 + 14.2 * static_cast<double>((tiles_of<FewParts>(a, v_lo) + 255) / 256) : 1e300;
+  const double least = std::min(std::min(large, medium), std::min(few, parts));
+  if (least == large) with<Large>(go);
+  else if (least == medium) past && rows <= 128 ? with<Fp8Cfg<C, 4 / C, 128, 2, 2, 2, 1, true>>(go) : with<Medium>(go);
+  else if (least == few) past && rows <= 64 ? with<Fp8Cfg<C, 2 / C, 128, 4, 1, 3, 1, true>>(go) : with<Few>(go);
+  else with<FewParts>(go);
 }
 template <class F>
 void choose(const LmHeadArgs& a, int v_lo, F&& go) {
