@@ -129,7 +129,8 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
   for (int i = 0; i < BL; ++i) {
     const int r = piece_row(BL, i);
-    bo[i] = static_cast<uint32_t>(min(max(w0 + r, f.v_lo), w_last) - w0) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(BL, i)) * 16;
+    // (differences: behind the last id of a table of 2^31 - 1 there is no number)
+    bo[i] = static_cast<uint32_t>(min(max(r, f.v_lo - w0), w_last - w0)) * static_cast<uint32_t>(d) + piece_chunk(odd_piece(BL, i)) * 16;
   }
   // scales of 16 rows x 4 blocks of k to a load
   const uint64_t sbase = reinterpret_cast<uint64_t>(f.h_scales) + static_cast<uint64_t>(h0) * G * 4;
@@ -187,10 +188,10 @@ __global__ __launch_bounds__(K::THREADS) __attribute__((amdgpu_waves_per_eu(2)))
   f16x8 op[2][NB + NC];                                   // operands of two MFMA steps
   f32x16 total[NC][NB], acc[K::ACC][NC][NB];
   // The wavefront's columns lie in one group of 128 of the table, or in two: those from `border` on have the second scale.
-  const int first = w0 + wc * K::CW, border = 128 - first % 128;
+  const int first = w0 + min(wc * K::CW, w_last - w0), border = 128 - first % 128;
   float scale[NB], scale2[NB], sw = 0.f, sw2 = 0.f;
-  const uint64_t wscales = reinterpret_cast<uint64_t>(f.W_scales) + static_cast<uint64_t>(min(first, w_last) / 128) * G * 4;
-  const int64_t more = min(first, w_last) / 128 < w_last / 128 ? G : 0;
+  const uint64_t wscales = reinterpret_cast<uint64_t>(f.W_scales) + static_cast<uint64_t>(first / 128) * G * 4;
+  const int64_t more = first / 128 < w_last / 128 ? G : 0;
   int block_k = rot;                                      // the block of the walk's t-th step
 #pragma unroll
   for (int c = 0; c < NC; ++c)
