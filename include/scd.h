@@ -423,7 +423,7 @@ int scd_lm_head_fp8(scd_ctx* ctx, const uint8_t* d_h, const float* d_h_scales, c
 int scd_step_fp8(scd_ctx* ctx, const uint8_t* d_h, const float* d_h_scales, const uint8_t* d_W, const float* d_W_scales, void* d_state);
 
 /* scd_lm_head_kernel_name of these two, which launch the same kernel: lm_head_fp8_kernel<Fp8Cfg<1 + CFG, blocks of 32 window rows, columns,
- * wavefronts along the columns, along the rows, stages, W past the caches>, groups of 128 ids may end among a wavefront's columns> (127 characters
+ * wavefronts along the columns, along the rows, stages, parts of k, W past the caches>, groups of 128 ids may end among a wavefront's columns> (127 characters
  * hold it). */
 int scd_lm_head_fp8_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
 
