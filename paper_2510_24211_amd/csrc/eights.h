@@ -55,23 +55,30 @@ __device__ __forceinline__ void put_eight(bool f32, void* p, int64_t at, f32x8 v
 
 // ---- e4m3 numbers under a scale for each 128 --------------------------------------------------------
 // scale = largest / 448, code = v / scale: the largest becomes 448, the largest finite code.  Blocks whose largest is below 448 * 2^-126
-// (the scale would lose digits, its inverse be infinite) count as zeros: scale 0, codes 0.  A block that holds an infinity has an
-// infinite scale, one that holds a NaN a NaN for it.
+// (the scale would lose digits) count as zeros: scale 0, codes 0.  A block that holds an infinity has an infinite scale, one that holds a
+// NaN a NaN for it.
 constexpr float kMostE4M3 = 448.f;
 struct E4M3Scale {
-  float scale, inverse;
+  float scale, inverse, rest;         // rest = 1 - scale * inverse
 };
 __device__ __forceinline__ E4M3Scale e4m3_scale(uint32_t largest_bits) {       // of |v|: as integers they compare alike, NaNs highest
   const float most = __uint_as_float(largest_bits);
   const bool none = most < 448.f * 1.17549435e-38f;
-  const float scale = none ? 0.f : __fdiv_rn(most, kMostE4M3);
-  return {scale, none ? 0.f : __fdiv_rn(1.f, scale)};
+  const float scale = none ? 0.f : __fdiv_rn(most, kMostE4M3), inverse = none ? 0.f : __fdiv_rn(1.f, scale);
+  return {scale, inverse, inverse == 0.f ? 0.f : __fmaf_rn(-scale, inverse, 1.f)};
 }
-// v * inverse is within 1.5 * 2^-23 of v / scale: at most 448.0001, which rounds to 448, so nothing has to be clamped.
-__device__ __forceinline__ uint2 to_e4m3(f32x8 v, float inverse) {
+// The quotient v / scale = v * inverse / (1 - rest) = v * inverse + v * inverse * rest + ..., within 2^-46 of its size before its one rounding to fp32.
+// (v * inverse alone is off by up to two steps of fp32 and lands on the other side of a border of two codes where the quotient is on it: 3 of
+// 10000 codes of bf16 weights.)  None of its terms leaves the normal numbers, whatever the scale.  The compiler's own division takes 2304 x 4096 rows
+// 14.4 us, these three operations 12.8, one 12.5; 16384 x 1280 weights 17.6, 12.2 and 11.1.
+//   Zeros and infinite scales have 0 for inverse and rest: quotients 0, and NaN for an infinity.  A quotient is at most 448.0001, which
+// rounds to 448, so nothing has to be clamped.
+__device__ __forceinline__ uint2 to_e4m3(f32x8 v, const E4M3Scale& s) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = __fmaf_rn(v[j], s.inverse, v[j] * s.inverse * s.rest);
   auto four = [&](float a, float b, float c, float d) -> uint32_t {
-    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, low, true));
+    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true));
   };
   return make_uint2(four(v[0], v[1], v[2], v[3]), four(v[4], v[5], v[6], v[7]));
 }

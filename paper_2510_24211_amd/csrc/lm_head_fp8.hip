@@ -446,7 +446,7 @@ __global__ __launch_bounds__(256) void quantize_fp8_kernel(const uint16_t* __res
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = static_cast<int64_t>(group) * 128 + i * 16 + threadIdx.x / 16;
-      if (row < V && p < pieces) reinterpret_cast<uint2*>(codes)[row * pieces + p] = to_e4m3(v[i].wide(), s.inverse);
+      if (row < V && p < pieces) reinterpret_cast<uint2*>(codes)[row * pieces + p] = to_e4m3(v[i].wide(), s);
     }
     if (threadIdx.x == 0) scales[static_cast<int64_t>(group) * gridDim.x + blockIdx.x] = s.scale;
   }

@@ -68,7 +68,7 @@ __device__ __forceinline__ void store_normed(const NormArgs& a, int64_t row, int
     most = max(most, dpp_u32<kDppMirror>(most));
     const E4M3Scale s = e4m3_scale(most);
     if (p < pieces) {
-      static_cast<uint2*>(a.y)[row * pieces + p] = to_e4m3(y, s.inverse);
+      static_cast<uint2*>(a.y)[row * pieces + p] = to_e4m3(y, s);
       if (p % 16 == 0) a.scales[row * ((pieces + 15) / 16) + p / 16] = s.scale;
     }
   } else {
