@@ -208,7 +208,8 @@ def _typed(t, numel, what):
 
 
 class TensorList:
-    """Tensors (contiguous, bf16 or fp32, views among them) as gradient_norm and clip_gradients take them; it keeps them alive."""
+    """Tensors (contiguous, bf16 or fp32, views among them) as gradient_norm and clip_gradients take them: the memory that they have now, which
+    the list keeps alive.  A tensor that has other memory later (its data exchanged, its storage resized) needs a new list: calls refuse this one."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -218,9 +219,18 @@ class TensorList:
             if p is None:
                 raise TypeError(f"tensor {i}: expected a CUDA tensor")
             self.array[i] = ScdTensor(p, t.numel(), _TYPE[t.dtype])
+        self._memory = [t.detach() for t in self.tensors]
+        self._addresses = [t.data_ptr() for t in self.tensors]
 
     def __len__(self):
         return len(self.tensors)
+
+    def check(self, what):
+        """Raises ValueError if a tensor's memory is not the one it had."""
+        now = [t.data_ptr() for t in self.tensors]
+        if now != self._addresses:
+            i = next(i for i, (a, b) in enumerate(zip(now, self._addresses)) if a != b)
+            raise ValueError(f"{what}: tensor {i} has other memory than when the list was made")
 
 
 class QuantizedWeights:
@@ -550,6 +560,7 @@ class Scd:
 
     def gradient_norm(self, grads, norm, workspace):
         """norm[0] = the 2-norm of all tensors of a TensorList together."""
+        grads.check("grads")
         self._check(self.lib.scd_gradient_norm(
             self.ctx, grads.array, len(grads), _ptr(norm, (torch.float32,), 1, "norm"), _ptr(workspace, (torch.uint8,), 1, "workspace"),
             workspace.numel()), "scd_gradient_norm")
@@ -558,6 +569,8 @@ class Scd:
         """out[i] = grads[i] * min(1, max_norm / norm[0]); out may be grads."""
         if len(grads) != len(out):
             raise ValueError(f"{len(out)} outputs for {len(grads)} tensors")
+        grads.check("grads")
+        out.check("out")
         self._check(self.lib.scd_clip_gradients(
             self.ctx, grads.array, out.array, len(grads), float(max_norm), _ptr(norm, (torch.float32,), 1, "norm")), "scd_clip_gradients")
 
