@@ -157,7 +157,7 @@ template <bool STREAM_F32, bool GRAD_F32, int T, int NV, int R>
 __global__ __launch_bounds__(256) void norm_backward_kernel(const NormBackwardArgs a) {
   constexpr int RW = 256 / T;          // rows side by side
   __shared__ float ex[2][R][4];
-  __shared__ float whole[T == 64 ? 4 * 64 * 8 : 1];
+  __shared__ f32x4 whole[T == 64 ? 4 * 64 * 2 : 1];
   const int t = threadIdx.x % T, pieces = a.d / 8, side = T == 64 ? wave_index() : 0;
   f32x8 gain[NV], dgain[NV];
 #pragma unroll
