@@ -433,7 +433,7 @@ int scd_lm_head_fp8_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
  * for n = 0), type a scd_type.  d_norm fp32, one element: written by scd_gradient_norm, read by scd_clip_gradients, which takes any norm that
  * the caller puts there (of several machines' gradients together, say).  out[i] has the elements of grads[i], in either type; it may be
  * the same tensor (of the same type: left alone where norm <= max_norm); otherwise nothing may overlap.  A norm that is infinite leaves
- * zeros (NaN where the gradient is infinite), one that is NaN makes all NaN.  max_norm >= 0.  Workspace as in scd_norm_backward. */
+ * zeros (NaN where the gradient is infinite), one that is NaN makes all NaN.  max_norm >= 0; infinite: finite norms leave the gradients as they are.  Workspace as in scd_norm_backward. */
 typedef struct scd_tensor {
   void* d;
   int64_t n;

@@ -148,7 +148,8 @@ __global__ __launch_bounds__(1024) void norm_of_parts_kernel(const double* __res
 
 __global__ __launch_bounds__(256) void clip_kernel(const Table t, float most, const float* __restrict__ norm) {
   const float have = norm[0];
-  const float by = have <= most ? 1.f : __fdiv_rn(most, have);        // (a NaN for a NaN)
+  // 0 under an infinite norm, whatever max_norm is; a NaN for a NaN
+  const float by = have == __builtin_inff() ? 0.f : have <= most ? 1.f : __fdiv_rn(most, have);
   const uint32_t chunks = t.first[t.count];
   for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
     const uint32_t c = chunks - 1 - i;
