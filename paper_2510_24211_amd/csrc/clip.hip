@@ -148,20 +148,23 @@ __global__ __launch_bounds__(1024) void norm_of_parts_kernel(const double* __res
 
 __global__ __launch_bounds__(256) void clip_kernel(const Table t, float most, const float* __restrict__ norm) {
   const float have = norm[0];
-  // 0 under an infinite norm, whatever max_norm is; a NaN for a NaN
-  const float by = have == __builtin_inff() ? 0.f : have <= most ? 1.f : __fdiv_rn(most, have);
+  // 0 under an infinite norm, whatever max_norm is; a NaN for a NaN.  Factors near or below the end of fp32's normal numbers, which would lose
+  // digits, are kept 2^128 times as large, with 2^-64 on either side of the product.
+  const bool whole = have <= most && have < __builtin_inff(), far = most < have * 0x1p-96f;
+  const float by = whole ? 1.f : have == __builtin_inff() ? 0.f : far ? __fdiv_rn(most * 0x1p64f, have * 0x1p-64f) : __fdiv_rn(most, have);
+  const float side = far ? 0x1p-64f : 1.f;
   const uint32_t chunks = t.first[t.count];
   for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
     const uint32_t c = chunks - 1 - i;
     const int k = tensor_of(t, c);
     const bool in_f32 = t.in_f32[k], out_f32 = t.out_f32[k];
     void* const out = t.out[k];
-    if (by == 1.f && out == t.in[k]) continue;       // (of one type then: nothing changes)
+    if (whole && out == t.in[k]) continue;           // (of one type then: nothing changes)
     const int64_t begin = static_cast<int64_t>(c - t.first[k]) * kChunk;
     auto go = [&](auto in_type, auto out_type) {
       constexpr bool IN = decltype(in_type)::value, OUT = decltype(out_type)::value;
-      over_chunk<IN>(t.in[k], t.n[k], begin, [&](f32x8 v, int64_t at) { put_any<OUT>(out, at, v * by); },
-                     [&](float v, int64_t at) { put_one<OUT>(out, at, v * by); });
+      over_chunk<IN>(t.in[k], t.n[k], begin, [&](f32x8 v, int64_t at) { put_any<OUT>(out, at, v * side * by * side); },
+                     [&](float v, int64_t at) { put_one<OUT>(out, at, v * side * by * side); });
     };
     if (in_f32) out_f32 ? go(TrueT{}, TrueT{}) : go(TrueT{}, FalseT{});
     else out_f32 ? go(FalseT{}, TrueT{}) : go(FalseT{}, FalseT{});

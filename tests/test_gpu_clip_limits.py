@@ -1,4 +1,6 @@
-"""Clipping under an infinite norm with any max_norm."""
+"""Clipping under an infinite norm with any max_norm, and where max_norm / norm is below the normal numbers of fp32.
+
+Tolerance as of the other clipping: factor and product one rounding of 2^-24 each, a step of the output's type, half of its smallest one."""
 import math
 
 import pytest
@@ -7,7 +9,10 @@ import torch
 from paper_2510_24211_amd import binding as B
 
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+U = 2.0 ** -24
+BF, F32 = torch.bfloat16, torch.float32
+HALF = {BF: 2.0 ** -8, F32: U}
+STEP = {BF: 2.0 ** -134, F32: 2.0 ** -150}
 
 
 def _ctx():
@@ -45,3 +50,20 @@ def test_no_limit_on_a_finite_norm_leaves_gradients_as_they_are(place):
     norm.fill_(math.nan)
     s.clip_gradients(ts, B.TensorList(out), math.inf, norm)
     assert all(t.isnan().all() for t in out)
+
+
+# factors below 2^-126, of 2^-149 and less, and of a max_norm that is itself below the normal numbers
+@pytest.mark.parametrize("most,norm", [(1e-3, 1e37), (1e-5, 3e38), (2.0 ** -20, 2.0 ** 110), (2.0 ** -140, 3.0), (2.0 ** -149, 1e-30), (3 * 2.0 ** -149, 1e-35),
+                                       (1e-12, 3e38), (1.0, 2.0 ** 97), (0.0, 2.0 ** -149), (1.0, 1e20)])
+@pytest.mark.parametrize("types", [(F32, F32), (F32, BF), (BF, BF), (BF, F32)])
+def test_factors_below_the_normal_numbers(most, norm, types):
+    s = _ctx()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(17003, device="cuda", generator=g) * torch.exp2(torch.randint(-140, 126, (17003,), device="cuda", generator=g).float())
+    x = x.to(types[0])
+    have = torch.full((1,), norm, device="cuda")
+    out = torch.full((17003,), 9.0, device="cuda").to(types[1])
+    s.clip_gradients(B.TensorList([x]), B.TensorList([out]), most, have)
+    most = torch.tensor(most, dtype=F32).double().item()
+    want = x.double() * (most / have.double().item())
+    assert ((out.double() - want).abs() <= (HALF[types[1]] + 4 * U) * want.abs() + STEP[types[1]]).all()
