@@ -428,7 +428,7 @@ int scd_step_fp8(scd_ctx* ctx, const uint8_t* d_h, const float* d_h_scales, cons
 int scd_lm_head_fp8_kernel_name(scd_ctx* ctx, char* host_buf, size_t cap);
 
 /* Norm of many gradients together, sqrt(sum of all elements' squares) (added up in 64 bits, stored as fp32), and clipping,
- *   out = g * min(1, max_norm / norm), rounded once.
+ *   out = g * min(1, max_norm / norm): the factor is rounded to fp32, the product to fp32 and from there to the output's type.
  * Arrays of `count` tensors in HOST memory, read during the call; a tensor's d is aligned to its elements, n >= 0 (up to 2^40; d may be NULL
  * for n = 0), type a scd_type.  d_norm fp32, one element: written by scd_gradient_norm, read by scd_clip_gradients, which takes any norm that
  * the caller puts there (of several machines' gradients together, say).  out[i] has the elements of grads[i], in either type; it may be
