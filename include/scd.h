@@ -402,6 +402,8 @@ int scd_norm_fp8(scd_ctx* ctx, const uint16_t* d_x, const void* d_residual, int3
 
 /* Gradient of both (of y as it is before its rounding) with respect to the rows and the gains:
  *   dx = inv * (a - s * inv^2 * mean(a * s)) + ds,  a = gain * dy;   dgain = sum over the rows of dy * s * inv
+ * Behind a bf16 stream s is the rounded sum and inv that of the sum before: dx's second term and the terms of dgain then carry the stream's
+ * rounding (up to 2^-8 of |s|), whatever types they are stored in; an fp32 stream keeps it out.
  *   d_sum (s: without a residual x, with stream_type SCD_BF16) and d_inv as scd_norm left them;  d_dy bf16 [rows, d];  d_dsum [rows, d] of
  * type grad_type: the gradient that reaches s from elsewhere, or NULL;  d_dx [rows, d] of type grad_type: the gradient of x and of the
  * residual alike; it may be d_dsum, or d_dy if it is bf16;  d_dgain [d] of type gain_grad_type, or NULL, added to with accumulate = 1 (in 32 bits,
