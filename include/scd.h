@@ -396,7 +396,7 @@ int scd_norm(scd_ctx* ctx, const uint16_t* d_x, const void* d_residual, int32_t 
 /* The same with y in 8 bits: d_codes e4m3 (4 exponent and 3 mantissa bits, no infinities) [rows, d] and d_scales fp32 [rows, ceil(d / 128)],
  *   scale = max |y| / 448 over 128 of a row,  code = y / scale (the quotient in fp32), rounded to the nearest, to the even one of two.
  * 128 values of which none reaches 448 * 2^-126 count as zeros (scale and codes 0); with an infinity among them the scale is infinite,
- * with a NaN a NaN. */
+ * with a NaN a NaN.  (scd_lm_head_fp8 reads rows of a multiple of 16 columns, this call writes any that the configuration allows.) */
 int scd_norm_fp8(scd_ctx* ctx, const uint16_t* d_x, const void* d_residual, int32_t stream_type, const void* d_gain, int32_t gain_type, float eps,
                  int32_t rows, uint8_t* d_codes, float* d_scales, void* d_sum, float* d_inv);
 

@@ -5,8 +5,9 @@
 // (they are exact there: no range is lost, and the unit that adds them is idle otherwise), the workgroups' sums in order by a last one.
 //   Bound by memory, each gradient being read twice: the norm has to be known first.  Clipping goes backwards, so that it begins with what the
 // norm's pass has left in the last cache, and stores past the caches, so that what it writes does not drive that out.  805 million bf16
-// gradients in 50 tensors into bf16: 841 us (4.83 GB: 5.7 TB/s) where forwards and through the caches took 940; 34 million fp32 ones into
-// bf16 62 us, 67 before.  512 workgroups of 64 KB at a time are as fast as any number up to 2048 (841 to 860 us), 4096 with 16 KB take 880.
+// gradients in 50 tensors into bf16: 841 us (4.83 GB: 5.7 TB/s) where forwards and through the caches took 940; in place 878, 297 with nothing
+// to clip; 34 million fp32 ones into bf16 62 us, 67 before.  512 workgroups of 64 KB at a time are as fast as any number up to 2048 (841 to
+// 860 us), 4096 with 16 KB take 880.
 #include <algorithm>
 
 #include "eights.h"

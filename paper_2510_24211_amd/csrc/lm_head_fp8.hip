@@ -13,11 +13,12 @@
 // load holds chunk (l % 8) ^ ((row >> 1) & 7): operand reads are then free of bank conflicts.  Scales of h come for four blocks at a time (a word
 // per row and block would ask the L2 for as many lines as h and W together: 5 % of the time), W's by way of the scalar cache.
 //
-//   What bounds it (d = 4096, guidance).  Few rows: memory.  One row x 65536 ids takes 45 us (268 MB of W: 6.0 TB/s), 32 x 2 rows 54; the bf16 head
-// takes 82 for the latter.  Many rows: the matrix pipes at the clock that they leave the card.  512 x 2 rows x 8192 ids, one round of tiles, take
-// 61 to 63 us; with every vector instruction and load taken out of the loop 52 to 54 remain, which is 1.43 PFLOP/s behind some 8 us of
-// launch, first loads and stores, the rate of a large product of 16 bits.  512 x 2 x 64000 takes 490 to 510 us (1.05 to 1.1 PFLOP/s).  What was
-// tried: loads and conversions ahead of the MFMAs instead of between them 541 us; the sums of a block carried over the loop's end as copies
+//   What bounds it (d = 4096, guidance).  Few rows: memory.  One row x 65536 ids takes 45 us (268 MB of W: 6.0 TB/s), 32 x 2 rows 51 to 56; the bf16 head
+// takes 82 for either.  Many rows: instructions.  512 x 2 rows x 8192 ids, one round of tiles, take 61 to 68 us (the bf16 head 61 to 63); with every vector
+// instruction and load taken out of the loop 52 to 54 remained, 48 of them products at 1.43 PFLOP/s, the rate of a large product of 16 bits, 4 to
+// 6 launch, first loads and stores.  512 x 2 x 64000 takes 490 to 518 us (1.04 to 1.1 PFLOP/s; the bf16 head 446 to 454): by counters the matrix pipes are
+// busy half of the time (42 % in 480 x 2 x 8191), 64 cycles of a SIMD pass for each MFMA of 32, and 7.4 other vector instructions of 4 stand beside it.
+//   What was tried: loads and conversions ahead of the MFMAs instead of between them 541 us; the sums of a block carried over the loop's end as copies
 // (64 moves, and spilled offsets whose reloads wait for all loads) 880; all workgroups from block 0 on 65 instead of 59 (32 x 2 rows);
 // logits turned in LDS for stores of whole lines: nothing; stores past the caches: 560.
 #include "eights.h"
@@ -396,14 +397,21 @@ void choose_of(const LmHeadArgs& a, int v_lo, F&& go) {
   const bool past = static_cast<int64_t>(a.n) * a.d >= (1 << 28);
   if constexpr (C == 1) {
     if (rows <= 32) {
+      // Four parts of k while every compute unit has a workgroup of them (d > 384: a block of k for each part), one part of twice as many beyond.
+      // One row, tables from memory, four parts and one (us): d = 512: 16384 ids 6.8 and 7.1, 16449 10.1 and 7.9, 32768 11.5 and 9.1; d = 1280: 8192 ids 8.7
+      // and 10.2, 16384 9.9 and 10.5, 16449 14.9 and 12.4, 32768 17.6 and 13.6, 65000 32 and 19; d = 4096: 8192 ids 13.8 and 22.5, 16384 18.0 and 23.2,
+      // 16449 26.8 and 28.2, 24000 29.1 and 29.3, 32768 33.0 and 30.2, 65000 60 and 53.  32 rows are alike; the choice is within 6 % of
+      // the better one everywhere.
       if (tiles_of<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(a, v_lo) <= 256 && a.d > 384) with<Fp8Cfg<1, 1, 64, 2, 1, 3, 4>>(go);
       else past ? with<Fp8Cfg<1, 1, 64, 2, 1, 3, 1, true>>(go) : with<Fp8Cfg<1, 1, 64, 2, 1, 3>>(go);
       return;
     }
   }
-  // What rounds of tiles over 256 compute units take, measured at d = 4096 (us, 64 to 512 rows with guidance x 500 to 8000 ids; at d = 1024 they stand
-  // to each other alike): a round of the larger shape 50 to 65, of two smaller tiles per compute unit 67, of one 35 to 42, of two streams 43, of
-  // one 26 to 30, of parts 14 each behind the first.  64 x 2 rows x 1000: 50, 35, 26, 14 us; 512 x 2 x 8000: 65, 67, 83, 111.
+  // What rounds of tiles over 256 compute units take, measured at d = 4096 (us, 64 to 512 rows with guidance x 500 to 8000 ids): a round of the larger
+  // shape 50 to 65, of two smaller tiles per compute unit 67, of one 35 to 42, of two streams 43, of one 26 to 30, of parts 14 each behind the
+  // first.  64 x 2 rows x 1000: 50, 35, 26, 14 us; 512 x 2 x 8000: 65, 67, 83, 111.  Other lengths stand to each other alike: at d = 1024 16, 12, 9, 7 and 21, 21,
+  // 25, 49 us, at d = 128 (no parts) 5.5, 5.2, 4.2 and 9.2, 8.9, 10.7.  Over 32 to 512 rows with guidance x 1000 to 16000 ids x d = 128 to 4096 the shape
+  // that is chosen is within 8 % of the best of the four.
   auto halves = [](int64_t tiles, double two, double one) {
     const int64_t rest = tiles % 512;
     return static_cast<double>(tiles / 512) * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
@@ -423,7 +431,8 @@ void choose(const LmHeadArgs& a, int v_lo, F&& go) {
 }
 
 // ---- weights in 8 bits ---------------------------------------------------------------------------------------------
-// A workgroup takes a block of 128 x 128 of the table: 16 lanes to a row, eight elements each, eight rows of a thread.
+// A workgroup takes a block of 128 x 128 of the table: 16 lanes to a row, eight elements each, eight rows of a thread.  Bound by memory: 65536 x 4096 take
+// 146 us (805 MB: 5.5 TB/s), 16384 x 1280 12.2.
 __global__ __launch_bounds__(256) void quantize_fp8_kernel(const uint16_t* __restrict__ W, int V, int d, uint8_t* __restrict__ codes,
                                                            float* __restrict__ scales) {
   __shared__ uint32_t ex[4];

@@ -4,9 +4,10 @@
 // Everything in fp32 (s is normed before it is rounded to the stream's type), each result rounded once.  The normed rows are stored as
 // bf16, or as e4m3 codes with a scale for each 128 of a row, which is what the LM head over 8-bit rows reads.  All of it moves
 // memory and computes little: a row is read once and kept in registers until it is written.
-//   Bound by memory: 25600 x 4096 rows in bf16 take 146 us (839 MB: 5.75 TB/s; a large copy reaches 5.1), 2304 x 4096 into 8 bits 12.5 us (66 MB), their
-// gradient 152 us (839 MB and 17 MB of the workgroups' sums: 5.6 TB/s).  Small calls are a launch: one row of 1280 takes 2.4 us on the
-// card, 515 rows of the gradient 5.2 and 3.8 us for the gains.
+//   Bound by memory: 25600 x 4096 rows in bf16 take 146 us (839 MB: 5.75 TB/s; a large copy reaches 5.1), 2304 x 4096 into 8 bits 12.8 us (66 MB), their
+// gradient 152 us (839 MB and 17 MB of the workgroups' sums: 5.6 TB/s), with dx and ds in fp32 225 (1.26 GB: 5.6).  Small calls are a launch: one row of 1280
+// takes 2.4 us on the card, 515 rows of the gradient 5.2 and 3.8 us for the gains.  Rows of more than 8192 columns are read twice: 4096 x 16384 take 111 us,
+// 98 into 8 bits, the gradient 151, 194 with fp32 (4.8, 4.8, 3.6 and 4.2 TB/s of what has to move).
 //   A row has a wavefront up to 1024 columns (no barrier; four rows to a workgroup), a workgroup beyond.
 #include <algorithm>
 
